@@ -1,0 +1,109 @@
+/*
+ * gptq_w4a16_serving.h - C ABI of the operators around the W4A16 matrix multiply in which every row of a batch picks
+ * weights of its own: mixture-of-experts layers on 4-bit experts, and low-rank adapters of many requests beside a shared
+ * 4-bit projection.
+ *
+ * Types, layouts, alignment (16 bytes), ownership, streams, errors and scratch are those of gptq_w4a16.h: device pointers,
+ * row-major contiguous tensors unless a row stride is named, calls that only enqueue, status codes (nothing is enqueued when
+ * one is returned), scratch of the library's own or of gptq_w4a16_set_workspace(), one per device.  No floating point
+ * atomics: the same inputs give the same bits.  Which row goes where is read on the GPU; no call waits for it.
+ */
+#ifndef GPTQ_W4A16_SERVING_H
+#define GPTQ_W4A16_SERVING_H
+
+#include "gptq_w4a16.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Type of the router's logits. */
+enum gptq_logits_type { GPTQ_LOGITS_FP16 = 0, GPTQ_LOGITS_FP32 = 1 };
+
+/*
+ * Routing: the top_k largest logits of every token, in descending order, the lower index first among equal ones.
+ *     logits   fp16 or fp32 [M, experts] (logits_type)
+ *     ids      int32 [M, top_k]       the chosen experts
+ *     weights  fp32  [M, top_k]       exp(l - max) / sum of the same over all experts of the row, or, with renormalize
+ *                                     non-zero, over the chosen ones; all in fp32
+ * An expert whose logit is -infinity or NaN is masked: it is never chosen and adds nothing to the sum.  Where fewer than
+ * top_k are left the remaining places hold the id -1 and the weight 0 (a row that masks all: every place).  Logits of
+ * +infinity share the weight among them.  1 <= experts <= 1024, 1 <= top_k <= min(experts, 32); else GPTQ_UNSUPPORTED_SHAPE.
+ */
+GPTQ_API int gptq_w4a16_moe_route(const void *logits, int logits_type, void *ids, void *weights, int M, int experts,
+                                  int top_k, int renormalize, gptq_stream_t stream);
+
+/*
+ * The packed weights of a layer's experts: the tensors of gptq_w4a16.h, one expert after the other.
+ *     gate_up_*  matrices [hidden, 2 * inter]: columns 0 .. inter-1 are the gate projection, the others the up projection
+ *                qweight int32 [experts, hidden/8, 2*inter], qzeros int32 [experts, hidden/group_size, inter/4],
+ *                scales fp16 [experts, hidden/group_size, 2*inter]
+ *     down_*     matrices [inter, hidden]: qweight int32 [experts, inter/8, hidden],
+ *                qzeros int32 [experts, inter/group_size, hidden/8], scales fp16 [experts, inter/group_size, hidden]
+ * group_size is a multiple of 32 that divides hidden and inter; every single matrix obeys the limits of gptq_w4a16.h.
+ */
+typedef struct gptq_w4a16_experts {
+    const void *gate_up_qweight, *gate_up_qzeros, *gate_up_scales;
+    const void *down_qweight, *down_qzeros, *down_scales;
+    int experts, hidden, inter, group_size;
+} gptq_w4a16_experts_t;
+
+/*
+ * A mixture-of-experts layer for few tokens:
+ *     out[m] = sum over j of weights[m, j] * ((silu(x[m] G_e) * (x[m] U_e)) D_e),   e = ids[m, j],  silu(v) = v / (1 + exp(-v))
+ * with x fp16 [M, hidden], ids int32 [M, top_k], weights fp32 [M, top_k], out fp16 [M, hidden].  An id outside
+ * [0, experts) - masked by the router, or an expert that lives on another GPU - adds nothing, whatever its weight; a token
+ * without any gets zeros.  Sums are fp32; the product of gate and up is rounded to fp16 (like any activation between two
+ * products of this library: values beyond 65504 become infinite), the result once.  Only experts that a token is sent to
+ * are read, once for every 32 of their tokens, so the call is meant for the tokens of decode steps: M * top_k <= 4096,
+ * top_k <= 32, experts <= 1024 (else GPTQ_UNSUPPORTED_SHAPE).
+ * `out` may not overlap x.
+ */
+GPTQ_API int gptq_w4a16_moe_experts(const void *x, const void *ids, const void *weights, const gptq_w4a16_experts_t *experts,
+                                    void *out, int M, int top_k, gptq_stream_t stream);
+
+/* The whole layer, gptq_w4a16_moe_route() and gptq_w4a16_moe_experts() in one call, with the limits of both. */
+GPTQ_API int gptq_w4a16_moe(const void *x, const void *logits, int logits_type, const gptq_w4a16_experts_t *experts,
+                            void *out, int M, int top_k, int renormalize, gptq_stream_t stream);
+
+/*
+ * Scratch that gptq_w4a16_moe() and gptq_w4a16_moe_experts() need of a caller-owned workspace (0 for invalid sizes).  As for
+ * gptq_w4a16_gemm(), library-owned scratch grows by itself, which is refused while `stream` is being captured
+ * (GPTQ_WORKSPACE_TOO_SMALL): make one eager call of the largest problem before capturing.
+ */
+GPTQ_API size_t gptq_w4a16_moe_workspace_bytes(int M, int hidden, int inter, int experts, int top_k, int group_size);
+
+/*
+ * Low-rank adapters of many requests:
+ *     out[m] = base[m] + scaling[l] * ((x[m] A_l^T) B_l^T),   l = adapter[m]
+ *     x        fp16  [M, K], rows ldx elements apart
+ *     a        fp16  [adapters, rank, K]     (adapters of a lower rank: padded with zeros)
+ *     b        fp16  [adapters, N, rank]
+ *     scaling  fp32  [adapters]
+ *     adapter  int32 [M]                     outside [0, adapters): the row has none, out[m] = base[m]
+ *     base     fp16  [M, N], rows ld_base elements apart
+ *     out      fp16  [M, N], rows ld_out elements apart; may be base itself (then ld_out == ld_base), no other overlap
+ * x A^T and all sums are kept in fp32, the result is rounded once.  K, N, rank and the row strides are multiples of 8 with
+ * ldx >= K, ld_base >= N, ld_out >= N; rank <= 256; adapters * rank * K and adapters * rank * N below 2^40.
+ */
+GPTQ_API int gptq_w4a16_lora_add(const void *x, const void *a, const void *b, const void *scaling, const void *adapter,
+                                 const void *base, void *out, int M, int K, int N, int rank, int adapters, int ldx,
+                                 int ld_base, int ld_out, gptq_stream_t stream);
+
+/*
+ * A shared projection with the adapters of its rows:  gptq_w4a16_gemm() of x (contiguous) to out, without g_idx, and
+ * gptq_w4a16_lora_add() on top of it.  (The product is rounded to fp16 before the adapters are added: it is the output that
+ * rows without an adapter get.  An act-order checkpoint: gptq_w4a16_gemm() or gptq_w4a16_gemm_prepared(), then
+ * gptq_w4a16_lora_add() in place.)
+ */
+GPTQ_API int gptq_w4a16_gemm_lora(const void *x, const void *qweight, const void *qzeros, const void *scales, const void *a,
+                                  const void *b, const void *scaling, const void *adapter, void *out, int M, int K, int N,
+                                  int group_size, int rank, int adapters, gptq_stream_t stream);
+
+/* Scratch that gptq_w4a16_gemm_lora(), and gptq_w4a16_lora_add() with group_size 0, need of a caller-owned workspace. */
+GPTQ_API size_t gptq_w4a16_lora_workspace_bytes(int M, int K, int N, int rank, int group_size);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* GPTQ_W4A16_SERVING_H */

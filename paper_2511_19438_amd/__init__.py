@@ -5,7 +5,7 @@ marshalling only); ``paper_2511_19438_amd.workloads`` draws the seeded synthetic
 Nothing here falls back to a CPU path: if the HIP library is missing the binding raises.
 """
 
-__all__ = ["binding", "workloads", "build"]
+__all__ = ["binding", "serving", "workloads", "build"]
 
 
 def __getattr__(name):

@@ -43,7 +43,11 @@ def units():
            ("skinny.hip", "skinny.o", []),
            ("mid.hip", "mid.o", []),
            ("act_order.hip", "act_order.o", []),
-           ("probe.hip", "probe.o", [])]
+           ("probe.hip", "probe.o", []),
+           ("serving.hip", "serving.o", []),
+           ("route.hip", "route.o", []),
+           ("experts.hip", "experts.o", []),
+           ("adapters.hip", "adapters.o", [])]
     for mb in DECODE_BATCHES:
         out.append(("decode_mb.hip", f"decode_mb{mb}.o", [f"-DGPTQ_DECODE_MB={mb}"]))
     for g in RING_GROUPS:

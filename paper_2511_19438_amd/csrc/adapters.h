@@ -1,0 +1,27 @@
+// Internal interface of the low-rank adapters (include/gptq_w4a16_serving.h).
+#pragma once
+
+#include "kernels.h"
+
+namespace gptq {
+namespace lora {
+
+constexpr int kMaxRank = 256;
+
+struct Call {
+    const half_t *x;         // [M, K], rows ldx apart
+    const half_t *a;         // [adapters, rank, K]
+    const half_t *b;         // [adapters, N, rank]
+    const float *scaling;    // [adapters]
+    const int32_t *adapter;  // [M]
+    const half_t *base;      // [M, N], rows ld_base apart
+    half_t *out;             // [M, N], rows ld_out apart
+    int M, K, N, rank, adapters, ldx, ld_base, ld_out;
+};
+
+// Bytes of scratch of a call: x A^T of every row, in K slices.
+size_t scratch_bytes(int M, int K, int rank);
+hipError_t launch_lora(const Call &c, void *scratch, hipStream_t stream);
+
+}  // namespace lora
+}  // namespace gptq

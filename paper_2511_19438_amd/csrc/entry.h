@@ -1,0 +1,36 @@
+// What the C-ABI translation units share: checks of arguments, scratch, and a product with scratch of its caller behind its own.
+#pragma once
+
+#include "gptq_w4a16.h"
+#include "kernels.h"
+
+namespace gptq {
+
+// Scratch of a launch: the block, and the slots of two-slice exchanges (exchange.h) behind it where the library owns it.
+// A caller's workspace has none: the same launches then exchange through partial sums, with the same result.
+struct Scratch {
+    void *ws = nullptr;
+    void *slots = nullptr;
+};
+
+inline bool aligned16(const void *p)
+{
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
+}
+
+inline size_t align256(size_t v)
+{
+    return (v + 255) & ~(size_t)255;
+}
+
+int check_shape(int K, int N, int group_size);
+int acquire_workspace(size_t bytes, hipStream_t stream, Scratch *out);
+
+// Validates the arguments of a GEMM call with the automatic plan and fills `p`.
+int check_gemm(const void *x, const void *qweight, const void *qzeros, const void *scales, void *out, int M, int K, int N,
+               int group_size, Problem &p);
+// The automatic product, in scratch that has `tail_bytes` of the caller's behind what the product uses: *tail.  Work that
+// uses the tail may be enqueued behind the product.
+int run_gemm_with_tail(const Problem &p, size_t tail_bytes, hipStream_t stream, void **tail);
+
+}  // namespace gptq

@@ -5,6 +5,7 @@
 #include <mutex>
 #include <vector>
 
+#include "entry.h"
 #include "kernels.h"
 
 namespace {
@@ -19,13 +20,6 @@ struct Workspace {
     void *ptr = nullptr;
     size_t bytes = 0;  // without the slots
     bool owned = false;
-};
-
-// Scratch of a launch: the block, and the slots of two-slice exchanges (exchange.h) behind it where the library owns it.
-// A caller's workspace has none: the same launches then exchange through partial sums, with the same result.
-struct Scratch {
-    void *ws = nullptr;
-    void *slots = nullptr;
 };
 
 std::mutex g_mutex;
@@ -64,12 +58,9 @@ int static_scratch_ptr(Scratch *out)
     return GPTQ_OK;
 }
 
-bool aligned16(const void *p)
-{
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
-}
+}  // namespace
 
-int check_shape(int K, int N, int group_size)
+int gptq::check_shape(int K, int N, int group_size)
 {
     if (K <= 0 || N <= 0 || group_size <= 0)
         return GPTQ_INVALID_ARG;
@@ -83,12 +74,16 @@ int check_shape(int K, int N, int group_size)
     return GPTQ_OK;
 }
 
+namespace {
+
 // Clears device memory and returns when that has happened: a memset of device memory may return before it is done, and
 // the streams that use the memory next need not wait for the null stream it runs on (hipStreamNonBlocking).
 bool clear_now(void *p, size_t bytes)
 {
     return hipMemset(p, 0, bytes) == hipSuccess && hipStreamSynchronize(nullptr) == hipSuccess;
 }
+
+}  // namespace
 
 // Makes sure the current device has scratch of at least `bytes`; returns it in *out.
 //
@@ -97,7 +92,7 @@ bool clear_now(void *p, size_t bytes)
 // sums, arrival counters, gathered activations).  A block that became too small is retired instead and stays
 // valid; retired blocks are released by gptq_w4a16_set_workspace().  Growth allocates and clears memory, which is
 // not allowed while `stream` is being captured: such a call is refused.
-int acquire_workspace(size_t bytes, hipStream_t stream, Scratch *out)
+int gptq::acquire_workspace(size_t bytes, hipStream_t stream, Scratch *out)
 {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices)
@@ -139,6 +134,8 @@ int acquire_workspace(size_t bytes, hipStream_t stream, Scratch *out)
     out->slots = static_cast<unsigned char *>(p) + want;
     return GPTQ_OK;
 }
+
+namespace {
 
 // Default kernel by batch size, from measurement on Llama-shaped layers.  A single row is streamed fastest
 // by the vector kernel.  From two rows on the small-batch MFMA kernel wins: its time is nearly flat up to 16
@@ -469,9 +466,22 @@ int run_gemm(const Problem &p, hipStream_t stream, const gptq_w4a16_plan_t *plan
     }
 }
 
-size_t align256(size_t v)
+// Scratch of the plan with `tail_bytes` behind it, at *tail; falls back to a plan that needs less where it cannot be had.
+// (The counter area at the front stays reserved even if this launch needs none: it must remain zero.)
+int acquire_with_tail(const Problem &p, Resolved &r, size_t tail_bytes, hipStream_t stream, Scratch *scratch, void **tail)
 {
-    return (v + 255) & ~(size_t)255;
+    for (;;) {
+        size_t kernel_bytes = align256(scratch_bytes(p, r));
+        if (kernel_bytes < decode_counter_bytes(p.N))
+            kernel_bytes = decode_counter_bytes(p.N);
+        const int rc = acquire_workspace(kernel_bytes + tail_bytes, stream, scratch);
+        if (rc == GPTQ_OK) {
+            *tail = static_cast<unsigned char *>(scratch->ws) + kernel_bytes;
+            return GPTQ_OK;
+        }
+        if (rc != GPTQ_WORKSPACE_TOO_SMALL || !fall_back(p, nullptr, r))
+            return rc;
+    }
 }
 
 int check_plan(const gptq_w4a16_plan_t *plan)
@@ -532,6 +542,20 @@ int make_problem(const void *x, const void *qweight, const void *qzeros, const v
 }
 
 }  // namespace
+
+int gptq::check_gemm(const void *x, const void *qweight, const void *qzeros, const void *scales, void *out, int M, int K, int N,
+                     int group_size, Problem &p)
+{
+    return make_problem(x, qweight, qzeros, scales, nullptr, out, M, K, N, group_size, nullptr, p);
+}
+
+int gptq::run_gemm_with_tail(const Problem &p, size_t tail_bytes, hipStream_t stream, void **tail)
+{
+    Resolved r = resolve(p, nullptr);
+    Scratch scratch;
+    const int rc = acquire_with_tail(p, r, tail_bytes, stream, &scratch, tail);
+    return rc == GPTQ_OK ? launch_resolved(p, r, scratch, stream) : rc;
+}
 
 extern "C" {
 
@@ -691,20 +715,12 @@ int gptq_w4a16_gemm_prepared(const void *x, const void *qweight_sorted, const vo
         return launch_resolved(p, r, scratch, st);
     }
     // scratch: what the kernel needs, then the gathered activations
-    // (the counter area at the front stays reserved even if this launch needs none: it must remain zero)
-    size_t kernel_bytes;
     Scratch scratch;
-    for (;;) {
-        kernel_bytes = align256(scratch_bytes(p, r));
-        if (kernel_bytes < decode_counter_bytes(N))
-            kernel_bytes = decode_counter_bytes(N);
-        const int wrc = acquire_workspace(kernel_bytes + (size_t)M * K * sizeof(half_t), st, &scratch);
-        if (wrc == GPTQ_OK)
-            break;
-        if (wrc != GPTQ_WORKSPACE_TOO_SMALL || !fall_back(p, nullptr, r))
-            return wrc;
-    }
-    half_t *xp = reinterpret_cast<half_t *>(static_cast<unsigned char *>(scratch.ws) + kernel_bytes);
+    void *tail = nullptr;
+    const int wrc = acquire_with_tail(p, r, (size_t)M * K * sizeof(half_t), st, &scratch, &tail);
+    if (wrc != GPTQ_OK)
+        return wrc;
+    half_t *xp = static_cast<half_t *>(tail);
     if (launch_gather_activations(static_cast<const half_t *>(x), static_cast<const int32_t *>(perm), xp, M, K, st) !=
         hipSuccess)
         return GPTQ_HIP_ERROR;

@@ -1,0 +1,237 @@
+// C-ABI entry points of include/gptq_w4a16_serving.h: argument validation, scratch, launches.
+#include "gptq_w4a16_serving.h"
+
+#include "adapters.h"
+#include "entry.h"
+#include "experts.h"
+
+namespace {
+
+using namespace gptq;
+
+int check_route(int M, int experts, int top_k)
+{
+    if (M <= 0 || experts <= 0 || top_k <= 0)
+        return GPTQ_INVALID_ARG;
+    if (experts > moe::kMaxExperts || top_k > moe::kMaxTopK || top_k > experts)
+        return GPTQ_UNSUPPORTED_SHAPE;
+    return GPTQ_OK;
+}
+
+// Sizes of a layer of experts.  A column tile of the output has an arrival counter: 65536 of 64 columns each.
+int check_layer(int M, int hidden, int inter, int experts, int top_k, int group_size)
+{
+    if (M <= 0 || hidden <= 0 || inter <= 0 || experts <= 0 || top_k <= 0 || group_size <= 0)
+        return GPTQ_INVALID_ARG;
+    if (experts > moe::kMaxExperts || top_k > moe::kMaxTopK || (long long)M * top_k > moe::kMaxPairs)
+        return GPTQ_UNSUPPORTED_SHAPE;
+    if (group_size % 32 || hidden % group_size || inter % group_size || hidden > (1 << 20) || inter > (1 << 20))
+        return GPTQ_UNSUPPORTED_SHAPE;
+    const int rc = check_shape(hidden, 2 * inter, group_size);
+    return rc != GPTQ_OK ? rc : check_shape(inter, hidden, group_size);
+}
+
+int check_experts(const gptq_w4a16_experts_t *e, int M, int top_k)
+{
+    if (!e || !e->gate_up_qweight || !e->gate_up_qzeros || !e->gate_up_scales || !e->down_qweight || !e->down_qzeros ||
+        !e->down_scales)
+        return GPTQ_INVALID_ARG;
+    const int rc = check_layer(M, e->hidden, e->inter, e->experts, top_k, e->group_size);
+    if (rc != GPTQ_OK)
+        return rc;
+    if (!aligned16(e->gate_up_qweight) || !aligned16(e->gate_up_qzeros) || !aligned16(e->gate_up_scales) ||
+        !aligned16(e->down_qweight) || !aligned16(e->down_qzeros) || !aligned16(e->down_scales))
+        return GPTQ_MISALIGNED;
+    return GPTQ_OK;
+}
+
+moe::Call make_call(const void *x, const gptq_w4a16_experts_t *e, void *out, int M, int top_k)
+{
+    moe::Call c = {};
+    c.x = static_cast<const half_t *>(x);
+    c.gate_up_qweight = static_cast<const uint32_t *>(e->gate_up_qweight);
+    c.gate_up_qzeros = static_cast<const uint32_t *>(e->gate_up_qzeros);
+    c.gate_up_scales = static_cast<const half_t *>(e->gate_up_scales);
+    c.down_qweight = static_cast<const uint32_t *>(e->down_qweight);
+    c.down_qzeros = static_cast<const uint32_t *>(e->down_qzeros);
+    c.down_scales = static_cast<const half_t *>(e->down_scales);
+    c.out = static_cast<half_t *>(out);
+    c.M = M;
+    c.hidden = e->hidden;
+    c.inter = e->inter;
+    c.experts = e->experts;
+    c.top_k = top_k;
+    c.group_size = e->group_size;
+    return c;
+}
+
+// The scratch of a layer: arrival counters, then what the layout says.
+int layer_scratch(const gptq_w4a16_experts_t *e, int M, int top_k, hipStream_t stream, moe::Layout &layout,
+                  unsigned *&counters, unsigned char *&rest)
+{
+    layout = moe::make_layout(M, e->hidden, e->inter, e->experts, top_k);
+    Scratch scratch;
+    const size_t front = decode_counter_bytes(e->hidden);
+    const int rc = acquire_workspace(front + layout.bytes, stream, &scratch);
+    counters = static_cast<unsigned *>(scratch.ws);
+    rest = static_cast<unsigned char *>(scratch.ws) + front;
+    return rc;
+}
+
+int check_lora(const void *x, const void *a, const void *b, const void *scaling, const void *adapter, const void *base,
+               const void *out, int M, int K, int N, int rank, int adapters, int ldx, int ld_base, int ld_out)
+{
+    if (!x || !a || !b || !scaling || !adapter || !base || !out || M <= 0 || K <= 0 || N <= 0 || rank <= 0 || adapters <= 0 ||
+        ldx < K || ld_base < N || ld_out < N || (base == out && ld_base != ld_out))
+        return GPTQ_INVALID_ARG;
+    if (K % 8 || N % 8 || rank % 8 || ldx % 8 || ld_base % 8 || ld_out % 8 || rank > lora::kMaxRank || K >= (1 << 23) ||
+        N >= (1 << 24) || (long long)adapters * rank * K >= (1ll << 40) || (long long)adapters * rank * N >= (1ll << 40))
+        return GPTQ_UNSUPPORTED_SHAPE;
+    if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(scaling) || !aligned16(adapter) || !aligned16(base) ||
+        !aligned16(out))
+        return GPTQ_MISALIGNED;
+    return GPTQ_OK;
+}
+
+int status(hipError_t err)
+{
+    return err == hipSuccess ? GPTQ_OK : GPTQ_HIP_ERROR;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gptq_w4a16_moe_route(const void *logits, int logits_type, void *ids, void *weights, int M, int experts, int top_k,
+                         int renormalize, gptq_stream_t stream)
+{
+    if (!logits || !ids || !weights || (logits_type != GPTQ_LOGITS_FP16 && logits_type != GPTQ_LOGITS_FP32))
+        return GPTQ_INVALID_ARG;
+    const int rc = check_route(M, experts, top_k);
+    if (rc != GPTQ_OK)
+        return rc;
+    if (!aligned16(logits) || !aligned16(ids) || !aligned16(weights))
+        return GPTQ_MISALIGNED;
+    return status(moe::launch_route(logits, logits_type == GPTQ_LOGITS_FP32, static_cast<int32_t *>(ids),
+                                    static_cast<float *>(weights), M, experts, top_k, renormalize != 0,
+                                    static_cast<hipStream_t>(stream)));
+}
+
+int gptq_w4a16_moe_experts(const void *x, const void *ids, const void *weights, const gptq_w4a16_experts_t *experts, void *out,
+                           int M, int top_k, gptq_stream_t stream)
+{
+    if (!x || !ids || !weights || !out)
+        return GPTQ_INVALID_ARG;
+    int rc = check_experts(experts, M, top_k);
+    if (rc != GPTQ_OK)
+        return rc;
+    if (!aligned16(x) || !aligned16(ids) || !aligned16(weights) || !aligned16(out))
+        return GPTQ_MISALIGNED;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    moe::Layout layout;
+    unsigned *counters;
+    unsigned char *scratch;
+    rc = layer_scratch(experts, M, top_k, st, layout, counters, scratch);
+    if (rc != GPTQ_OK)
+        return rc;
+    moe::Call c = make_call(x, experts, out, M, top_k);
+    c.ids = static_cast<const int32_t *>(ids);
+    c.weights = static_cast<const float *>(weights);
+    return status(moe::launch_experts(c, layout, scratch, counters, st));
+}
+
+int gptq_w4a16_moe(const void *x, const void *logits, int logits_type, const gptq_w4a16_experts_t *experts, void *out, int M,
+                   int top_k, int renormalize, gptq_stream_t stream)
+{
+    if (!x || !logits || !out || (logits_type != GPTQ_LOGITS_FP16 && logits_type != GPTQ_LOGITS_FP32))
+        return GPTQ_INVALID_ARG;
+    int rc = check_experts(experts, M, top_k);
+    if (rc != GPTQ_OK)
+        return rc;
+    rc = check_route(M, experts->experts, top_k);
+    if (rc != GPTQ_OK)
+        return rc;
+    if (!aligned16(x) || !aligned16(logits) || !aligned16(out))
+        return GPTQ_MISALIGNED;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    moe::Layout layout;
+    unsigned *counters;
+    unsigned char *scratch;
+    rc = layer_scratch(experts, M, top_k, st, layout, counters, scratch);
+    if (rc != GPTQ_OK)
+        return rc;
+    int32_t *ids = reinterpret_cast<int32_t *>(scratch + layout.ids);
+    float *weights = reinterpret_cast<float *>(scratch + layout.weights);
+    moe::Call c = make_call(x, experts, out, M, top_k);
+    c.ids = ids;
+    c.weights = weights;
+    const hipError_t err = moe::launch_route(logits, logits_type == GPTQ_LOGITS_FP32, ids, weights, M, experts->experts,
+                                             top_k, renormalize != 0, st);
+    return status(err != hipSuccess ? err : moe::launch_experts(c, layout, scratch, counters, st));
+}
+
+size_t gptq_w4a16_moe_workspace_bytes(int M, int hidden, int inter, int experts, int top_k, int group_size)
+{
+    if (check_layer(M, hidden, inter, experts, top_k, group_size) != GPTQ_OK)
+        return 0;
+    return decode_counter_bytes(hidden) + moe::make_layout(M, hidden, inter, experts, top_k).bytes;
+}
+
+int gptq_w4a16_lora_add(const void *x, const void *a, const void *b, const void *scaling, const void *adapter,
+                        const void *base, void *out, int M, int K, int N, int rank, int adapters, int ldx, int ld_base,
+                        int ld_out, gptq_stream_t stream)
+{
+    const int rc = check_lora(x, a, b, scaling, adapter, base, out, M, K, N, rank, adapters, ldx, ld_base, ld_out);
+    if (rc != GPTQ_OK)
+        return rc;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    // the counter area at the front of the scratch stays as it is
+    const size_t front = decode_counter_bytes(N);
+    Scratch scratch;
+    const int wrc = acquire_workspace(front + lora::scratch_bytes(M, K, rank), st, &scratch);
+    if (wrc != GPTQ_OK)
+        return wrc;
+    const lora::Call c = {static_cast<const half_t *>(x), static_cast<const half_t *>(a), static_cast<const half_t *>(b),
+                          static_cast<const float *>(scaling), static_cast<const int32_t *>(adapter),
+                          static_cast<const half_t *>(base), static_cast<half_t *>(out), M, K, N, rank, adapters, ldx,
+                          ld_base, ld_out};
+    return status(lora::launch_lora(c, static_cast<unsigned char *>(scratch.ws) + front, st));
+}
+
+int gptq_w4a16_gemm_lora(const void *x, const void *qweight, const void *qzeros, const void *scales, const void *a,
+                         const void *b, const void *scaling, const void *adapter, void *out, int M, int K, int N,
+                         int group_size, int rank, int adapters, gptq_stream_t stream)
+{
+    Problem p;
+    int rc = check_gemm(x, qweight, qzeros, scales, out, M, K, N, group_size, p);
+    if (rc != GPTQ_OK)
+        return rc;
+    rc = check_lora(x, a, b, scaling, adapter, out, out, M, K, N, rank, adapters, K, N, N);
+    if (rc != GPTQ_OK)
+        return rc;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    void *t = nullptr;
+    rc = run_gemm_with_tail(p, lora::scratch_bytes(M, K, rank), st, &t);
+    if (rc != GPTQ_OK)
+        return rc;
+    const lora::Call c = {p.x, static_cast<const half_t *>(a), static_cast<const half_t *>(b),
+                          static_cast<const float *>(scaling), static_cast<const int32_t *>(adapter), p.out, p.out, M, K, N,
+                          rank, adapters, K, N, N};
+    return status(lora::launch_lora(c, t, st));
+}
+
+size_t gptq_w4a16_lora_workspace_bytes(int M, int K, int N, int rank, int group_size)
+{
+    if (M <= 0 || K <= 0 || N <= 0 || rank <= 0 || K % 8 || N % 8 || rank % 8 || rank > lora::kMaxRank || group_size < 0)
+        return 0;
+    size_t front = decode_counter_bytes(N);
+    if (group_size > 0) {
+        const size_t product = gptq_w4a16_workspace_bytes(M, K, N, group_size);
+        if (check_shape(K, N, group_size) != GPTQ_OK)
+            return 0;
+        front = align256(product) > front ? align256(product) : front;
+    }
+    return front + lora::scratch_bytes(M, K, rank);
+}
+
+}  // extern "C"

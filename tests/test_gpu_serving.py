@@ -1,0 +1,324 @@
+"""Routing, expert layers and low-rank adapters against their definitions in 64 bits (GPU)."""
+import numpy as np
+import pytest
+import torch
+
+from tests.serving_reference import U16, experts64, lora64, random_packed, route64
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2511_19438_amd import serving
+
+    serving._load()
+    return serving
+
+
+def cuda(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def inside(got, want, off, what):
+    diff = np.abs(got.astype(np.float64) - want)
+    bad = ~(diff <= off)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} outside, worst {np.nanmax(diff / np.maximum(off, 1e-300))} of the bound"
+
+
+# ---- routing ----
+
+def route(S, logits, top_k, renormalize):
+    M = logits.shape[0]
+    ids = torch.full((M, top_k), -77, dtype=torch.int32, device="cuda")
+    weights = torch.full((M, top_k), 77.0, device="cuda")
+    S.gptq_w4a16_moe_route(cuda(logits), ids, weights, renormalize)
+    return ids.cpu().numpy(), weights.cpu().numpy()
+
+
+def check_route(S, logits, top_k, renormalize):
+    ids, weights = route(S, logits, top_k, renormalize)
+    want_ids, want = route64(logits, top_k, renormalize)
+    np.testing.assert_array_equal(ids, want_ids)
+    # expf and the division are good to a few units in the last place, a sum of up to 1024 shares to 22 additions' worth;
+    # shares below the smallest normal number may be lost
+    assert np.all(np.abs(weights - want) <= 40 * 2.0 ** -24 * want + 2.0 ** -120)
+
+
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+@pytest.mark.parametrize("M,E,top_k", [(1, 1, 1), (1, 8, 2), (5, 8, 8), (3, 63, 4), (7, 64, 6), (2, 65, 32), (9, 160, 8),
+                                       (4, 256, 8), (6, 257, 5), (3, 1024, 32), (1027, 60, 4)])
+def test_route(S, dtype, M, E, top_k):
+    rng = np.random.default_rng([M, E, top_k])
+    logits = (3 * rng.standard_normal((M, E))).astype(dtype)
+    for renormalize in (False, True):
+        check_route(S, logits, top_k, renormalize)
+
+
+@pytest.mark.parametrize("E", [4, 64, 100, 300])
+def test_route_ties_go_to_the_lower_index(S, E):
+    rng = np.random.default_rng(E)
+    logits = rng.integers(-1, 2, size=(33, E)).astype(np.float32)
+    logits[0] = 0.0
+    logits[1] = np.where(np.arange(E) % 2, 0.0, -0.0)  # zeros of both signs are equal
+    logits[2] = -np.finfo(np.float32).max              # a mask of the lowest value is still a number
+    logits[3] = -65504.0
+    for renormalize in (False, True):
+        check_route(S, logits, min(E, 7), renormalize)
+
+
+@pytest.mark.parametrize("E", [8, 64, 200, 1000])
+def test_route_masks_infinities_and_nan(S, E):
+    rng = np.random.default_rng(E)
+    logits = rng.standard_normal((12, E)).astype(np.float32)
+    logits[0] = -np.inf                                   # nothing left
+    logits[1, :] = np.nan
+    logits[2, 1:] = -np.inf                               # one left
+    logits[3, rng.random(E) < 0.7] = -np.inf
+    logits[4, rng.random(E) < 0.5] = np.nan
+    logits[5, [1, 4]] = np.inf                            # two infinities share
+    logits[6, 3], logits[6, 5] = np.inf, np.nan
+    logits[7] = np.where(np.arange(E) % 3 == 0, -np.finfo(np.float32).max, -np.inf)
+    logits[8] *= 1e30                                     # shares that underflow
+    for renormalize in (False, True):
+        check_route(S, logits, min(E, 6), renormalize)
+        with np.errstate(over="ignore"):
+            check_route(S, np.clip(logits, -np.inf, np.inf).astype(np.float16), min(E, 6), renormalize)
+
+
+# ---- experts ----
+
+def layer(rng, hidden, inter, experts, group):
+    return random_packed(rng, hidden, 2 * inter, group, experts), random_packed(rng, inter, hidden, group, experts)
+
+
+def run_experts(S, x, ids, weights, gate_up, down, group):
+    out = torch.full((x.shape[0], down[0].shape[2]), float("nan"), dtype=torch.float16, device="cuda")
+    S.gptq_w4a16_moe_experts(cuda(x), cuda(ids), cuda(weights), tuple(map(cuda, gate_up)), tuple(map(cuda, down)), out, group)
+    return out.cpu().numpy()
+
+
+def check_experts(S, x, ids, weights, gate_up, down, group, what=""):
+    got = run_experts(S, x, ids, weights, gate_up, down, group)
+    want, off = experts64(x, ids, weights, gate_up, down)
+    inside(got, want, off, f"experts {what}")
+    if want.size >= 512 and np.abs(want).any():
+        # roundings of the activation and of the output: independent, 2^-11 / sqrt(3) each at most
+        assert np.linalg.norm(got - want) <= 1.5 * U16 * np.linalg.norm(want)
+    return got
+
+
+SHAPES = [  # M, hidden, inter, experts, top_k, group
+    (1, 32, 32, 1, 1, 32), (1, 128, 128, 4, 2, 128), (2, 256, 96, 8, 8, 32), (3, 96, 192, 5, 3, 96), (8, 384, 128, 4, 2, 128),
+    (9, 160, 352, 6, 2, 32), (16, 1152, 384, 8, 2, 128), (17, 320, 256, 3, 2, 64), (31, 256, 512, 2, 2, 256),
+    (33, 224, 160, 3, 3, 32), (48, 128, 128, 4, 1, 128), (64, 640, 256, 8, 2, 128), (65, 192, 64, 64, 6, 32),
+    (130, 128, 256, 4, 4, 64), (257, 64, 64, 16, 8, 64), (4096, 32, 32, 2, 1, 32)]
+
+
+@pytest.mark.parametrize("M,hidden,inter,experts,top_k,group", SHAPES)
+def test_experts(S, M, hidden, inter, experts, top_k, group):
+    rng = np.random.default_rng([M, hidden, inter])
+    gate_up, down = layer(rng, hidden, inter, experts, group)
+    x = rng.standard_normal((M, hidden)).astype(np.float16)
+    ids = np.argsort(rng.random((M, experts)), 1)[:, :top_k].astype(np.int32)
+    weights = rng.random((M, top_k)).astype(np.float32)
+    check_experts(S, x, ids, weights, gate_up, down, group)
+
+
+@pytest.mark.parametrize("M", [1, 5, 16, 40, 100])
+@pytest.mark.parametrize("pattern", ["none", "one", "same", "duplicates", "outside", "few"])
+def test_experts_by_pattern(S, M, pattern):
+    hidden, inter, experts, top_k, group = 256, 128, 6, 3, 64
+    rng = np.random.default_rng([M, len(pattern)])
+    gate_up, down = layer(rng, hidden, inter, experts, group)
+    x = rng.standard_normal((M, hidden)).astype(np.float16)
+    weights = rng.standard_normal((M, top_k)).astype(np.float32)
+    ids = rng.integers(0, experts, size=(M, top_k)).astype(np.int32)
+    if pattern == "none":
+        ids[:] = -1
+    elif pattern == "one":
+        ids[:] = -1
+        ids[M // 2, 1] = 4
+    elif pattern == "same":
+        ids[:] = 2
+    elif pattern == "outside":
+        ids[rng.random(ids.shape) < 0.5] = experts
+        ids[rng.random(ids.shape) < 0.2] = 2 ** 31 - 1
+        ids[rng.random(ids.shape) < 0.2] = -2 ** 31
+        weights[(ids < 0) | (ids >= experts)] = np.nan  # of no one
+    elif pattern == "few":
+        ids[rng.random(ids.shape) < 0.8] = -1
+    got = run_experts(S, x, ids, weights, gate_up, down, group)
+    want, off = experts64(x, ids, np.where((ids >= 0) & (ids < experts), weights, 0).astype(np.float32), gate_up, down)
+    inside(got, want, off, pattern)
+    empty = ((ids < 0) | (ids >= experts)).all(1)
+    assert not got[empty].any()
+
+
+def test_a_row_of_infinities_leaves_the_others_alone(S):
+    M, hidden, inter, experts, top_k, group = 20, 256, 128, 4, 2, 128
+    rng = np.random.default_rng(5)
+    gate_up, down = layer(rng, hidden, inter, experts, group)
+    x = rng.standard_normal((M, hidden)).astype(np.float16)
+    ids = rng.integers(0, experts, size=(M, top_k)).astype(np.int32)
+    weights = rng.random((M, top_k)).astype(np.float32)
+    clean = check_experts(S, x, ids, weights, gate_up, down, group)
+    for bad in (np.inf, np.nan):
+        x2 = x.copy()
+        x2[3] = bad
+        got = run_experts(S, x2, ids, weights, gate_up, down, group)
+        keep = np.arange(M) != 3
+        np.testing.assert_array_equal(got[keep], clean[keep])
+
+
+@pytest.mark.parametrize("M,E,top_k,dtype", [(1, 8, 2, np.float16), (4, 8, 2, np.float32), (20, 30, 4, np.float16),
+                                             (64, 4, 2, np.float32), (100, 70, 3, np.float16), (300, 300, 2, np.float32)])
+def test_whole_layer(S, M, E, top_k, dtype):
+    hidden, inter, group = 128, 96, 32
+    rng = np.random.default_rng([M, E])
+    gate_up, down = layer(rng, hidden, inter, E, group)
+    x = rng.standard_normal((M, hidden)).astype(np.float16)
+    logits = rng.standard_normal((M, E)).astype(dtype)
+    logits[0, :] = -np.inf if M > 1 else logits[0, :]
+    for renormalize in (False, True):
+        out = torch.full((M, hidden), float("nan"), dtype=torch.float16, device="cuda")
+        S.gptq_w4a16_moe(cuda(x), cuda(logits), tuple(map(cuda, gate_up)), tuple(map(cuda, down)), out, top_k, group, renormalize)
+        ids, weights = route(S, logits, top_k, renormalize)
+        parts = run_experts(S, x, ids, weights, gate_up, down, group)
+        np.testing.assert_array_equal(out.cpu().numpy(), parts)  # the whole is its two parts, bit for bit
+        want_ids, want_weights = route64(logits, top_k, renormalize)
+        want, off = experts64(x, want_ids, want_weights, gate_up, down)
+        inside(parts, want, off * 1.01, "layer")
+
+
+def test_experts_repeat_bit_for_bit_on_another_stream_and_in_a_graph(S):
+    M, hidden, inter, experts, top_k, group = 24, 512, 256, 8, 2, 128
+    rng = np.random.default_rng(9)
+    gate_up, down = (tuple(map(cuda, t)) for t in layer(rng, hidden, inter, experts, group))
+    x = cuda(rng.standard_normal((M, hidden)).astype(np.float16))
+    logits = cuda(rng.standard_normal((M, experts)).astype(np.float16))
+    out = torch.empty(M, hidden, dtype=torch.float16, device="cuda")
+    S.gptq_w4a16_moe(x, logits, gate_up, down, out, top_k, group)
+    first = out.clone()
+    for _ in range(20):
+        out.fill_(float("nan"))
+        S.gptq_w4a16_moe(x, logits, gate_up, down, out, top_k, group)
+        assert torch.equal(out, first)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out.fill_(float("nan"))
+        S.gptq_w4a16_moe(x, logits, gate_up, down, out, top_k, group)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out, first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        S.gptq_w4a16_moe(x, logits, gate_up, down, out, top_k, group)
+    for seed in range(4):  # other tokens and other experts in every replay
+        x.copy_(torch.randn_like(x, dtype=torch.float32))
+        logits.copy_(torch.randn_like(logits, dtype=torch.float32))
+        eager = torch.empty_like(out)
+        S.gptq_w4a16_moe(x, logits, gate_up, down, eager, top_k, group)
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+
+
+# ---- adapters ----
+
+def adapters(rng, count, rank, K, N):
+    return ((rng.standard_normal((count, rank, K)) / np.sqrt(K)).astype(np.float16),
+            (0.1 * rng.standard_normal((count, N, rank))).astype(np.float16), rng.uniform(-2, 2, count).astype(np.float32))
+
+
+def run_lora(S, x, a, b, scaling, adapter, base):
+    out = torch.full(base.shape, float("nan"), dtype=torch.float16, device="cuda")
+    S.gptq_w4a16_lora_add(cuda(x), cuda(a), cuda(b), cuda(scaling), cuda(adapter), cuda(base), out)
+    return out.cpu().numpy()
+
+
+@pytest.mark.parametrize("which", ["mixed", "none", "same", "own", "outside", "packed"])
+@pytest.mark.parametrize("M,K,N,rank,count", [
+    (1, 8, 8, 8, 1), (1, 256, 128, 16, 4), (2, 520, 72, 8, 3), (15, 264, 200, 24, 4), (16, 1024, 136, 64, 7), (17, 96, 264, 16, 3),
+    (33, 1032, 64, 40, 5), (64, 512, 512, 16, 64), (65, 128, 328, 128, 2), (77, 2752, 88, 256, 2), (130, 64, 1032, 32, 9),
+    (300, 160, 96, 88, 6)])
+def test_lora(S, which, M, K, N, rank, count):
+    rng = np.random.default_rng([M, K, N, rank])
+    a, b, scaling = adapters(rng, count, rank, K, N)
+    x = rng.standard_normal((M, K)).astype(np.float16)
+    base = rng.standard_normal((M, N)).astype(np.float16)
+    adapter = rng.integers(-1, count, size=M).astype(np.int32)
+    if which == "none":
+        adapter[:] = -1
+    elif which == "same":
+        adapter[:] = count - 1
+    elif which == "own":
+        adapter[:] = np.arange(M) % count
+    elif which == "outside":
+        adapter[rng.random(M) < 0.4] = count
+        adapter[rng.random(M) < 0.2] = -2 ** 31
+        adapter[rng.random(M) < 0.2] = 2 ** 31 - 1
+    elif which == "packed":
+        adapter = np.sort(adapter)
+    got = run_lora(S, x, a, b, scaling, adapter, base)
+    want, off = lora64(x, a, b, scaling, adapter, base)
+    inside(got, want, off, which)
+
+
+def test_lora_on_columns_of_wider_matrices_and_in_place(S):
+    M, K, N, rank, count = 21, 264, 136, 16, 4
+    rng = np.random.default_rng(3)
+    a, b, scaling = adapters(rng, count, rank, K, N)
+    wide_x = rng.standard_normal((M, K + 24)).astype(np.float16)
+    wide = rng.standard_normal((M, 3 * N)).astype(np.float16)
+    adapter = rng.integers(-1, count, size=M).astype(np.int32)
+    x = cuda(wide_x)[:, 8:8 + K]
+    target = cuda(wide)
+    view = target[:, N:2 * N]
+    S.gptq_w4a16_lora_add(x, cuda(a), cuda(b), cuda(scaling), cuda(adapter), view, view)
+    got = target.cpu().numpy()
+    want, off = lora64(wide_x[:, 8:8 + K], a, b, scaling, adapter, wide[:, N:2 * N])
+    inside(got[:, N:2 * N], want, off, "in place")
+    np.testing.assert_array_equal(got[:, :N], wide[:, :N])
+    np.testing.assert_array_equal(got[:, 2 * N:], wide[:, 2 * N:])
+
+
+def test_lora_infinite_adapters_stay_with_their_rows(S):
+    M, K, N, rank, count = 18, 128, 64, 16, 3
+    rng = np.random.default_rng(4)
+    a, b, scaling = adapters(rng, count, rank, K, N)
+    x = rng.standard_normal((M, K)).astype(np.float16)
+    base = rng.standard_normal((M, N)).astype(np.float16)
+    adapter = (np.arange(M) % 4 - 1).astype(np.int32)
+    clean = run_lora(S, x, a, b, scaling, adapter, base)
+    a2, b2, x2 = a.copy(), b.copy(), x.copy()
+    a2[1, 3], b2[1, 5], x2[7] = np.inf, np.nan, np.nan
+    keep = (adapter != 1) & (np.arange(M) != 7)
+    got = run_lora(S, x2, a2, b2, scaling, adapter, base)
+    np.testing.assert_array_equal(got[keep], clean[keep])
+    # sums beyond fp16's range between the two products are no harm: x A is kept in fp32
+    x3 = (x * 300).astype(np.float16)
+    a3, b3 = (a * 400).astype(np.float16), (b * 1e-3).astype(np.float16)
+    got = run_lora(S, x3, a3, b3, scaling, adapter, base)
+    want, off = lora64(x3, a3, b3, scaling, adapter, base)
+    assert np.abs(x3.astype(np.float64) @ a3[0].astype(np.float64).T).max() > 65504
+    inside(got, want, off, "large sums")
+
+
+@pytest.mark.parametrize("M,K,N,group,rank,count", [(1, 512, 264, 128, 16, 3), (5, 256, 136, 64, 8, 5), (32, 1024, 520, 128, 16, 32),
+                                                    (40, 384, 264, 32, 24, 4), (200, 512, 264, 128, 32, 4)])
+def test_gemm_lora_is_the_product_with_the_adapters_on_top(S, M, K, N, group, rank, count):
+    from paper_2511_19438_amd import binding
+
+    rng = np.random.default_rng([M, K, N])
+    packed = tuple(map(cuda, random_packed(rng, K, N, group)))
+    a, b, scaling = adapters(rng, count, rank, K, N)
+    x = rng.standard_normal((M, K)).astype(np.float16)
+    adapter = rng.integers(-1, count, size=M).astype(np.int32)
+    out = torch.full((M, N), float("nan"), dtype=torch.float16, device="cuda")
+    S.gptq_w4a16_gemm_lora(cuda(x), *packed, cuda(a), cuda(b), cuda(scaling), cuda(adapter), out, group)
+    base = torch.empty_like(out)
+    binding.gptq_w4a16_gemm(cuda(x), *packed, None, base, group)
+    want, off = lora64(x, a, b, scaling, adapter, base.cpu().numpy())
+    inside(out.cpu().numpy(), want, off, "gemm_lora")
