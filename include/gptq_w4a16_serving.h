@@ -56,7 +56,8 @@ typedef struct gptq_w4a16_experts {
  * without any gets zeros.  Sums are fp32; the product of gate and up is rounded to fp16 (like any activation between two
  * products of this library: values beyond 65504 become infinite), the result once.  Only experts that a token is sent to
  * are read, once for every 32 of their tokens, so the call is meant for the tokens of decode steps: M * top_k <= 4096,
- * top_k <= 32, experts <= 1024 (else GPTQ_UNSUPPORTED_SHAPE).
+ * top_k <= 32, experts <= 1024, hidden and inter <= 2^20, M * hidden and M * top_k * inter < 2^31 (else
+ * GPTQ_UNSUPPORTED_SHAPE).
  * `out` may not overlap x.
  */
 GPTQ_API int gptq_w4a16_moe_experts(const void *x, const void *ids, const void *weights, const gptq_w4a16_experts_t *experts,

@@ -32,6 +32,7 @@ COMMON = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc"
 DECODE_BATCHES = (1, 2, 4, 8, 16)
 PREFILL_TILES = (1, 3, 5, 8, 9, 10, 11, 12, 13, 14)
 RING_GROUPS = (1, 2, 4)
+EXPERTS_SCALINGS = (0, 1, 2)
 
 
 def units():
@@ -52,6 +53,10 @@ def units():
         out.append(("decode_mb.hip", f"decode_mb{mb}.o", [f"-DGPTQ_DECODE_MB={mb}"]))
     for g in RING_GROUPS:
         out.append(("ring.hip", f"ring{g}.o", [f"-DGPTQ_RING_GPU={g}"]))
+    for s in EXPERTS_SCALINGS:
+        for d in (0, 1):
+            out.append(("experts_scale.hip", f"experts_scale{s}_{d}.o",
+                        [f"-DGPTQ_EXPERTS_SCALING={s}", f"-DGPTQ_EXPERTS_DOWN={d}"]))
     for t in PREFILL_TILES:
         out.append(("prefill_tile.hip", f"prefill_tile{t}.o", [f"-DGPTQ_PREFILL_TILE={t}"]))
     return out

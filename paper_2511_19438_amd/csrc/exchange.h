@@ -49,13 +49,13 @@
 namespace gptq {
 
 // Thread 0 of a workgroup, after s_waitcnt vmcnt(0) in every wavefront and the barrier that follows the
-// workgroup's partial stores: returns the number of workgroups that had arrived before.
-__device__ __forceinline__ unsigned slice_arrive(unsigned *counter)
+// workgroup's partial stores: returns the number of workgroups (or of what else `count` counts) that had arrived before.
+__device__ __forceinline__ unsigned slice_arrive(unsigned *counter, unsigned count = 1u)
 {
 #if GPTQ_FORMAL_EXCHANGE_FENCES
-    return __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
+    return __hip_atomic_fetch_add(counter, count, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
 #else
-    return __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return __hip_atomic_fetch_add(counter, count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #endif
 }
 

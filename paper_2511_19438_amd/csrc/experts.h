@@ -10,15 +10,20 @@ constexpr int kMaxExperts = 1024;
 constexpr int kMaxTopK = 32;
 constexpr int kMaxPairs = 4096;  // (token, place) pairs of a call
 
-// A unit of work: up to `rows` tokens of one expert.
+constexpr int kUnitRows = 32;  // at most
+
+// A unit of work: up to kUnitRows (token, place) pairs of one expert.  The pairs stand in the unit itself: a workgroup finds
+// out all that it has to know in one round trip to memory.
 struct Unit {
-    int expert, first, count, unused;  // pairs[first .. first + count)
+    int expert, count, unused[2];
+    int32_t pairs[kUnitRows];  // token * top_k + place
 };
 
 // What the GPU found out about a call, at the front of its scratch (behind the arrival counters).
 struct Grouping {
     int units;  // in use; <= max_units()
-    int unused[3];
+    int pairs;  // with an expert
+    int unused[2];
 };
 
 // Units of `rows` rows that `pairs` pairs over `experts` experts can make at most: every expert's last may be short.
@@ -29,28 +34,28 @@ inline int max_units(int pairs, int experts, int rows)
 
 // Scratch of a call, as offsets from its start.
 struct Layout {
-    size_t grouping, units, pairs, ids, weights, hidden, partial, bytes;
+    size_t grouping, units, ids, weights, hidden, partial, bytes;
 };
 
 struct Call {
     const half_t *x;        // [M, hidden]
-    const int32_t *ids;     // [M, top_k]
-    const float *weights;   // [M, top_k]
+    int32_t *ids;           // [M, top_k]: read, or with logits: scratch that they are left in
+    float *weights;         // [M, top_k]
+    const void *logits;     // [M, experts] or null
+    bool logits_fp32, renormalize;
     const uint32_t *gate_up_qweight, *gate_up_qzeros, *down_qweight, *down_qzeros;
     const half_t *gate_up_scales, *down_scales;
     half_t *out;            // [M, hidden]
     int M, hidden, inter, experts, top_k, group_size;
 };
 
-// Rows of a unit for a call.
-int unit_rows(int M, int experts, int top_k);
 Layout make_layout(int M, int hidden, int inter, int experts, int top_k);
 
 hipError_t launch_route(const void *logits, bool fp32, int32_t *ids, float *weights, int M, int experts, int top_k,
                         bool renormalize, hipStream_t stream);
 // Groups the pairs of ids [M, top_k] by expert.
 hipError_t launch_group(const int32_t *ids, int pairs, int experts, int rows, Grouping *grouping, Unit *units,
-                        int32_t *order, hipStream_t stream);
+                        hipStream_t stream);
 hipError_t launch_experts(const Call &c, const Layout &l, unsigned char *scratch, unsigned *counters, hipStream_t stream);
 
 }  // namespace moe

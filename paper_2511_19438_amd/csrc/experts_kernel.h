@@ -1,0 +1,539 @@
+// The products of a mixture-of-experts layer on 4-bit weights, gfx950: one kernel for gate and up (with the activation
+// between) and for down (with the sum over a token's experts).
+//
+// A workgroup multiplies up to MAXROWS tokens of one expert with COLS columns of that expert's matrix; its wavefronts split K,
+// and their sums meet in LDS.  Every wavefront streams its share of K through a ring of LDS slots of 64 k that DMA fills:
+// packed words, the tokens' activations (gathered by the DMA's addresses), scales and zero points.  How many rows of
+// activations travel, and how many 16-row blocks are multiplied, goes by the number of tokens that the expert has.  The
+// arithmetic is that of the small-batch kernel (ring_kernel.h): the B operand is the exact q - z in fp16, a group's sum is
+// scaled in fp32.
+//
+// Gate and up.  The columns of a workgroup are COLS / 2 of the gate projection and the COLS / 2 of the up projection beside
+// them, so that silu(gate) * up is formed where both sums meet and goes out once, in fp16: what the next product takes.
+//
+// Down.  A token's experts are different workgroups; each leaves the fp32 sums of its pairs in scratch and counts itself in at
+// its column tile, and the last of a tile adds every token's experts in the order of their places (exchange.h).
+#pragma once
+
+#include "exchange.h"
+#include "experts.h"
+#include "lds_dma.h"
+#include "route_token.h"
+#include "skinny_kernel.h"
+
+namespace gptq {
+namespace moe {
+
+using skinny::NibbleMagic;
+using skinny::as_half2;
+using skinny::u32x4_t;
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// How a workgroup finds out what it has to do.
+enum Mode {
+    kOneToken,  // M = 1: workgroups for every place of the token; its expert is read, or found here from the router's logits
+    kDirect,    // few pairs and experts: workgroups for every expert, which look through all ids for its pairs
+    kGrouped    // units of work made by launch_group()
+};
+
+constexpr int kDirectPairs = 512;  // pairs that a workgroup looks through at most
+
+struct Args {
+    const half_t *x;         // gate and up: [M, K], the tokens; down: [pairs, K], their activations
+    const uint32_t *qweight; // [experts, K/8, N]
+    const uint32_t *qzeros;
+    const half_t *scales;
+    const Grouping *grouping;  // kGrouped
+    const Unit *units;
+    int32_t *ids;            // [M, top_k]
+    float *weights;
+    const void *logits;      // kOneToken, gate and up: [experts] of which ids and weights are found and left, or null
+    half_t *hidden;          // gate and up: [pairs, N/2]
+    float *partial;          // down: [pairs, N]
+    half_t *out;             // down: [M, N]
+    unsigned *counters;      // down: one per column tile, zero between launches
+    int M, top_k, K, N, group_size, experts, tiles, mode, chunks, logits_fp32, renormalize;
+};
+
+// What a launch is made of.
+struct Shape {
+    int rows;    // of a workgroup at a time: 8, 16 or 32
+    bool wide;   // 128 columns (gate and up) or 64 (down) of a workgroup, four wavefronts; else 64, or 32 and eight wavefronts
+    int groups;  // of workgroups, one for each tile
+};
+
+template <int SCALING, bool DOWN>
+hipError_t launch_product(const Args &a, const Shape &s, hipStream_t stream);
+
+// How often the sums are scaled, by the group size.
+enum Scaling {
+    kPairs,   // groups of 128 n: every two stages of 64 k, which share a row of scales
+    kStages,  // groups of 64 n: every stage
+    kSteps    // groups of 32 n: every 32 k; K may end in the middle of a stage
+};
+
+template <int COLS, int LX, Scaling SC>
+struct Slot {
+    static constexpr int W_BYTES = COLS * 32;            // [8 packed rows][COLS] words
+    static constexpr int X_BYTES = LX * 1024;            // [8 LX rows][64] halves, 16-byte chunks swizzled
+    static constexpr int SZ_LOADS = COLS <= 96 ? 1 : 2;  // of one group: COLS / 2 + COLS / 8 words
+    static constexpr int SZ_BYTES = SZ_LOADS * 256;      // scales [COLS] halves, zero words [COLS / 8], padding
+    static constexpr int ROWS_SZ = SC == kSteps ? 2 : 1;
+    static constexpr int BYTES = W_BYTES + X_BYTES + ROWS_SZ * SZ_BYTES;
+};
+
+template <int TM, int LX, int COLS, int WAVES, Scaling SC, int DEPTH>
+constexpr size_t lds_bytes()
+{
+    const size_t ring = (size_t)WAVES * DEPTH * Slot<COLS, LX, SC>::BYTES, sums = (size_t)WAVES * 16 * TM * COLS * 4;
+    return ring > sums ? ring : sums;
+}
+
+// Column of the matrix of a tile's column c, for a load of `width` columns; those past the last are read at the last and not
+// stored.
+template <int COLS, bool DOWN>
+__device__ __forceinline__ int column(int tile, int c, int width, int N)
+{
+    if (DOWN)
+        return min(tile * COLS + c, N - width);
+    const int half = COLS / 2;
+    return c < half ? min(tile * half + c, N / 2 - width) : N / 2 + min(tile * half + c - half, N / 2 - width);
+}
+
+// The sums of `count` pairs with the tile's columns, over each wavefront's share of K: red [WAVES][ROWS][COLS].
+// TM: 16-row blocks; LX: DMA instructions of the activations (8 rows each).  Rows past the last pair repeat it.
+template <int TM, int LX, int COLS, int WAVES, Scaling SC, int DEPTH, bool DOWN>
+__device__ __forceinline__ void stream_weights(const Args &a, int expert, int tile, const int32_t *pairs, int count,
+                                               unsigned char *smem)
+{
+    constexpr int ROWS = 16 * TM;
+    constexpr int NF = COLS / 64, NH = COLS % 64 / 32;  // a lane's columns: NF times four, NH times two
+    constexpr int NT = 4 * NF + 2 * NH;
+    using S = Slot<COLS, LX, SC>;
+    constexpr int LW = S::W_BYTES / 1024;
+    constexpr int LS = S::ROWS_SZ * S::SZ_LOADS;
+    constexpr int UNIT = SC == kPairs ? 2 : 1;  // stages between two rows of scales
+    constexpr int LOADS0 = LW + LX + LS, LOADS1 = LW + LX + (UNIT == 2 ? 0 : LS);
+    constexpr int XROWS = 8 * LX;
+    constexpr int QUADS = COLS / 4;
+    static_assert(DEPTH == 2 || DEPTH == 3, "the waits below");
+    static_assert(COLS == 32 || COLS == 64 || COLS == 128, "whole DMA instructions, whole zero words on both sides");
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int cq = lane & 15;
+    const int kg = lane >> 4;
+    const int K = a.K, N = a.N;
+    const int stages = (K + 63) / 64;
+    const int blocks = stages / UNIT;  // (kPairs: K is a multiple of 128)
+    const int per_wave = (blocks + WAVES - 1) / WAVES;
+    const int b0 = min(wave * per_wave, blocks), b1 = min(b0 + per_wave, blocks);
+
+    // ---- DMA sources: a wavefront-uniform base that advances from stage to stage and a byte offset per lane ----
+    uint32_t off_w[LW], off_w_last[LW];  // (last: a stage whose second half is past K repeats its first)
+#pragma unroll
+    for (int q = 0; q < LW; ++q) {
+        const int chunk = q * 64 + lane;  // of the stage's 8 packed rows, QUADS chunks each
+        const uint32_t row = chunk / QUADS, col = column<COLS, DOWN>(tile, 4 * (chunk % QUADS), 4, N);
+        off_w[q] = (row * N + col) * 4u;
+        off_w_last[q] = ((row & 3) * N + col) * 4u;
+    }
+    uint32_t off_x[LX], off_x_last[LX];
+#pragma unroll
+    for (int q = 0; q < LX; ++q) {
+        const int row = 8 * q + (lane >> 3);
+        const int pair = pairs[min(row, count - 1)];
+        const uint32_t chunk = (lane & 7) ^ (row >> 1 & 7);
+        const uint32_t base = (uint32_t)(DOWN ? pair : pair / a.top_k) * K;
+        off_x[q] = (base + chunk * 8) * 2u;
+        off_x_last[q] = (base + (chunk & 3) * 8) * 2u;
+    }
+    const size_t groups = K / a.group_size;
+    const uint32_t *const qweight = a.qweight + (size_t)expert * (K / 8) * N;
+    const char *w_next = reinterpret_cast<const char *>(qweight + (size_t)b0 * UNIT * 8 * N);
+    const char *x_next = reinterpret_cast<const char *>(a.x + (size_t)b0 * UNIT * 64);
+    const size_t w_step = (size_t)N * 32;
+    // scales and zero points: the row of scales of the next step that needs one, and its place in its group, in 32 k
+    const int per_group = a.group_size / 32;
+    constexpr int kSpan = SC == kPairs ? 4 : SC == kStages ? 2 : 1;  // steps that one load of a row serves
+    int group = b0 * UNIT * 2 / per_group;
+    int in_group = b0 * UNIT * 2 - group * per_group;
+    const char *sz_next[S::SZ_LOADS];
+    uint32_t sz_step[S::SZ_LOADS];
+#pragma unroll
+    for (int j = 0; j < S::SZ_LOADS; ++j) {
+        const int i = 64 * j + lane;
+        const bool scales = i < COLS / 2;
+        const int n = scales ? column<COLS, DOWN>(tile, 2 * i, 2, N) : column<COLS, DOWN>(tile, 8 * min(i - COLS / 2, COLS / 8 - 1), 8, N);
+        const size_t at = ((size_t)expert * groups + group) * N + n;
+        sz_next[j] = scales ? reinterpret_cast<const char *>(a.scales + at) : reinterpret_cast<const char *>(a.qzeros + at / 8);
+        sz_step[j] = scales ? (uint32_t)N * 2u : (uint32_t)N / 2u;
+    }
+
+    const unsigned char *const ring = smem + (size_t)wave * (DEPTH * S::BYTES);
+    const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(
+        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)ring);
+    int left = (b1 - b0) * UNIT;  // stages whose loads have not been issued
+    const int last_half = SC == kSteps && K % 64 != 0 && b1 == blocks;  // the last of them ends after 32 k
+    uint32_t put = ring_lds;
+    auto issue = [&](bool first_of_unit) {
+        const bool half = SC == kSteps && last_half && left == 1;
+#pragma unroll
+        for (int q = 0; q < LW; ++q)
+            dma_16(put + q * 1024, half ? off_w_last[q] : off_w[q], w_next);
+        if (UNIT == 1 || first_of_unit) {
+#pragma unroll
+            for (int g = 0; g < S::ROWS_SZ; ++g) {
+                in_group += kSpan;
+                bool step = in_group == per_group;
+                in_group = step ? 0 : in_group;
+                if (half && g == 0)  // nothing behind it: the second row is the first again
+                    step = false;
+#pragma unroll
+                for (int j = 0; j < S::SZ_LOADS; ++j) {
+                    dma_4(put + S::W_BYTES + S::X_BYTES + g * S::SZ_BYTES + j * 256, sz_next[j]);
+                    sz_next[j] += step ? sz_step[j] : 0u;
+                }
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < LX; ++q)
+            dma_16(put + S::W_BYTES + q * 1024, half ? off_x_last[q] : off_x[q], x_next);
+        w_next += w_step;
+        x_next += 128;
+        put += S::BYTES;
+        put = put == ring_lds + DEPTH * S::BYTES ? ring_lds : put;
+        --left;
+    };
+
+    // ---- operand addresses inside a slot ----
+    uint32_t a_off[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int row = 16 * i + cq < XROWS ? 16 * i + cq : cq % (XROWS < 16 ? XROWS : 16);
+        a_off[i] = (uint32_t)S::W_BYTES + row * 128u + ((uint32_t)(kg ^ (row >> 1 & 7)) << 4);
+    }
+    struct Words {
+        u32x4_t f[NF > 0 ? NF : 1];
+        u32x2_t h;
+    };
+    auto read_step = [&](const unsigned char *slot, int st, Words &w, u32x4_t (&x)[TM]) {
+        const unsigned char *row = slot + (4 * st + kg) * (COLS * 4);
+#pragma unroll
+        for (int b = 0; b < NF; ++b)
+            w.f[b] = *reinterpret_cast<const u32x4_t *>(row + b * 256 + cq * 16);
+        if (NH)
+            w.h = *reinterpret_cast<const u32x2_t *>(row + NF * 256 + cq * 8);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+            x[i] = *reinterpret_cast<const u32x4_t *>(slot + (a_off[i] ^ (uint32_t)(st << 6)));
+    };
+
+    float4_t acc[TM][NT];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            acc[i][t] = float4_t{0.f, 0.f, 0.f, 0.f};
+    const NibbleMagic magic;
+    constexpr int SPG = SC == kPairs ? 4 : SC == kStages ? 2 : 1;  // steps between scalings
+
+    if (b0 < b1) {
+        int todo = (b1 - b0) * UNIT;  // stages that have not been consumed
+#pragma unroll
+        for (int i = 0; i < DEPTH - 1; ++i)
+            if (UNIT == 2 || left > 0)
+                issue(i % UNIT == 0);
+        uint32_t get = 0;
+        for (int b = b0; b < b1; ++b) {
+            float4_t d[TM][NT];
+            half2_t neg_lo[NT], neg_hi[NT];
+            float sf[NT];
+#pragma unroll
+            for (int s = 0; s < UNIT; ++s) {
+                // The stage has arrived once no more than the loads of the stages issued after it are outstanding.
+                if (left > 0) {
+                    issue((s + DEPTH - 1) % UNIT == 0);
+                    if (DEPTH == 3)
+                        wait_loads<LOADS0 + LOADS1>();
+                    else if (s == 0)
+                        wait_loads<LOADS1>();
+                    else
+                        wait_loads<LOADS0>();
+                } else if (DEPTH == 3 && todo > 1) {
+                    if (s == 0)
+                        wait_loads<LOADS1>();
+                    else
+                        wait_loads<LOADS0>();
+                } else {
+                    wait_loads<0>();
+                }
+                --todo;
+                const bool half = SC == kSteps && last_half && todo == 0;
+                const unsigned char *slot = ring + get;
+                Words w[2];
+                u32x4_t x[2][TM];
+                read_step(slot, 0, w[0], x[0]);
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    if (st == 1 && half)
+                        break;
+                    const int step = 2 * s + st;  // of the unit
+                    if (step % SPG == 0) {        // a group begins: its zero points and scales
+                        const unsigned char *sz = slot + S::W_BYTES + S::X_BYTES + (SC == kSteps ? st : 0) * S::SZ_BYTES;
+#pragma unroll
+                        for (int c = 0; c < NF + NH; ++c) {
+                            const int col = c < NF ? c * 64 + 4 * cq : NF * 64 + 2 * cq;
+                            const uint32_t zeros =
+                                *reinterpret_cast<const uint32_t *>(sz + COLS * 2 + (col >> 3) * 4) >> (4 * (col & 7));
+                            uint32_t pair[2];
+                            pair[0] = *reinterpret_cast<const uint32_t *>(sz + col * 2);
+                            pair[1] = c < NF ? *reinterpret_cast<const uint32_t *>(sz + col * 2 + 4) : 0u;
+#pragma unroll
+                            for (int j = 0; j < (c < NF ? 4 : 2); ++j) {
+                                const uint32_t z = zeros >> (4 * j) & 15u;
+                                const uint32_t zz = z | (z << 16);
+                                neg_lo[4 * c + j] = as_half2(zz | 0xE400E400u);         // (-(1024 + z)) x2
+                                neg_hi[4 * c + j] = as_half2((zz << 4) | 0xD400D400u);  // (-(64 + z)) x2
+                                const uint16_t bits = (uint16_t)((j & 1) ? pair[j / 2] >> 16 : pair[j / 2] & 0xffffu);
+                                sf[4 * c + j] = (float)__builtin_bit_cast(half_t, bits);
+                            }
+                        }
+                    }
+                    if (st == 0) {
+                        read_step(slot, 1, w[1], x[1]);  // in flight under this step's arithmetic
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    half8_t av[TM];
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) {  // the k order of the weights: halves (0,4) (1,5) (2,6) (3,7)
+                        const u32x4_t xv = x[st][i];
+                        const u32x4_t xp = {__builtin_amdgcn_perm(xv[2], xv[0], 0x05040100u),
+                                            __builtin_amdgcn_perm(xv[2], xv[0], 0x07060302u),
+                                            __builtin_amdgcn_perm(xv[3], xv[1], 0x05040100u),
+                                            __builtin_amdgcn_perm(xv[3], xv[1], 0x07060302u)};
+                        av[i] = __builtin_bit_cast(half8_t, xp);
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint32_t word = t < 4 * NF ? w[st].f[t < 4 * NF ? t / 4 : 0][t % 4] : w[st].h[t % 2];
+                        const uint32_t w8 = word >> 8;
+                        const half2_t c0 = as_half2((word & magic.mask_lo) | magic.bias_lo) + neg_lo[t];
+                        const half2_t c1 = as_half2((word & magic.mask_hi) | magic.bias_hi) + neg_hi[t];
+                        const half2_t c2 = as_half2((w8 & magic.mask_lo) | magic.bias_lo) + neg_lo[t];
+                        const half2_t c3 = as_half2((w8 & magic.mask_hi) | magic.bias_hi) + neg_hi[t];
+                        const half8_t bv = half8_t{c0[0], c0[1], c1[0], c1[1], c2[0], c2[1], c3[0], c3[1]};
+                        const float4_t zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int i = 0; i < TM; ++i)
+                            d[i][t] =
+                                __builtin_amdgcn_mfma_f32_16x16x32_f16(av[i], bv, step % SPG == 0 ? zero : d[i][t], 0, 0, 0);
+                    }
+                    if (step % SPG == SPG - 1) {  // scale the sum
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    acc[i][t][r] = __builtin_fmaf(sf[t], d[i][t][r], acc[i][t][r]);
+                    }
+                }
+                get += S::BYTES;
+                get = get == (uint32_t)(DEPTH * S::BYTES) ? 0u : get;
+                // the next turn fills this slot again: its reads have to be done, used or not
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+
+    // ---- the wavefronts meet in LDS (in the place of the rings: every DMA has landed) ----
+    float *red = reinterpret_cast<float *>(smem);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float *row = red + ((size_t)wave * ROWS + 16 * i + 4 * kg + r) * COLS;
+#pragma unroll
+            for (int c = 0; c < NF; ++c)
+                *reinterpret_cast<float4_t *>(row + c * 64 + 4 * cq) =
+                    float4_t{acc[i][4 * c][r], acc[i][4 * c + 1][r], acc[i][4 * c + 2][r], acc[i][4 * c + 3][r]};
+            if (NH)
+                *reinterpret_cast<f32x2_t *>(row + NF * 64 + 2 * cq) = f32x2_t{acc[i][4 * NF][r], acc[i][4 * NF + 1][r]};
+        }
+}
+
+// One workgroup: the tokens of one expert (at most MAXROWS at a time) times COLS columns of its matrix.
+template <int MAXROWS, int COLS, int WAVES, Scaling SC, int DEPTH, bool DOWN>
+__global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
+{
+    constexpr int kThreads = 64 * WAVES;
+    constexpr int QUADS = COLS / 4;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ int32_t s_pairs[WAVES][MAXROWS];  // every wavefront finds the pairs for itself
+    __shared__ int s_last;
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int N = a.N;
+    const int tile = blockIdx.x % a.tiles, u = blockIdx.x / a.tiles;
+    const int all_pairs = a.M * a.top_k;
+    int32_t *const pairs = s_pairs[wave];
+
+    int expert = 0, found = 0, total_pairs = 0;  // of the workgroup's group; of the call
+    int first = 0, step = MAXROWS;               // found pairs that this workgroup begins with, and goes on by
+    int32_t id[kDirectPairs / 64];               // kDirect: a lane's ids
+    if (a.mode == kOneToken) {
+        int32_t mine;
+        if (!DOWN && a.logits) {
+            float weight;
+            int chosen;
+            if (a.logits_fp32)
+                route_any(static_cast<const float *>(a.logits), a.experts, a.top_k, a.renormalize, lane, chosen, weight);
+            else
+                route_any(static_cast<const half_t *>(a.logits), a.experts, a.top_k, a.renormalize, lane, chosen, weight);
+            mine = chosen;
+            if (blockIdx.x == 0 && tid < a.top_k) {
+                a.ids[tid] = chosen;
+                a.weights[tid] = weight;
+            }
+        } else {
+            mine = lane < a.top_k ? a.ids[lane] : -1;
+        }
+        const bool valid = lane < a.top_k && mine >= 0 && mine < a.experts;
+        total_pairs = __popcll(__ballot(valid));
+        expert = __builtin_amdgcn_readlane(mine, u);
+        found = __ballot(valid) >> u & 1 ? 1 : 0;
+        if (lane == 0)
+            pairs[0] = u;
+    } else if (a.mode == kDirect) {
+        expert = u / a.chunks;
+        first = (u - expert * a.chunks) * MAXROWS;
+        step = a.chunks * MAXROWS;
+#pragma unroll
+        for (int i = 0; i < kDirectPairs / 64; ++i)
+            id[i] = 64 * i + lane < all_pairs ? a.ids[64 * i + lane] : -1;
+#pragma unroll
+        for (int i = 0; i < kDirectPairs / 64; ++i) {
+            found += __popcll(__ballot(id[i] == expert));
+            total_pairs += __popcll(__ballot(id[i] >= 0 && id[i] < a.experts));
+        }
+    } else {
+        total_pairs = a.grouping->pairs;
+        if (u < a.grouping->units) {
+            const Unit &unit = a.units[u];
+            expert = __builtin_amdgcn_readfirstlane(unit.expert);
+            found = __builtin_amdgcn_readfirstlane(unit.count);
+            if (lane < MAXROWS)
+                pairs[lane] = unit.pairs[min(lane, found - 1)];
+        }
+    }
+    // (down: without any pair one workgroup of every tile still writes the zeros)
+    if (first >= found && !(DOWN && total_pairs == 0 && u == 0))
+        return;
+
+    float *const red = reinterpret_cast<float *>(smem);
+    int done = 0;
+    for (; first < found; first += step) {
+        const int count = min(found - first, MAXROWS);
+        if (a.mode == kDirect) {
+            int before = 0;
+#pragma unroll
+            for (int i = 0; i < kDirectPairs / 64; ++i) {
+                const uint64_t match = __ballot(id[i] == expert);
+                const int place = before + __popcll(match & ((1ull << lane) - 1)) - first;
+                if (id[i] == expert && place >= 0 && place < count)
+                    pairs[place] = 64 * i + lane;
+                before += __popcll(match);
+            }
+        }
+        if (done)
+            __syncthreads();  // the sums of the pairs before have been read
+        if (MAXROWS <= 8 || count <= 8)
+            stream_weights<1, 1, COLS, WAVES, SC, DEPTH, DOWN>(a, expert, tile, pairs, count, smem);
+        else if (MAXROWS <= 16 || count <= 16)
+            stream_weights<1, MAXROWS <= 8 ? 1 : 2, COLS, WAVES, SC, DEPTH, DOWN>(a, expert, tile, pairs, count, smem);
+        else if (count <= 24)
+            stream_weights<MAXROWS <= 16 ? 1 : 2, MAXROWS <= 16 ? 1 : 3, COLS, WAVES, SC, DEPTH, DOWN>(a, expert, tile, pairs,
+                                                                                                       count, smem);
+        else
+            stream_weights<MAXROWS <= 16 ? 1 : 2, MAXROWS <= 16 ? 1 : 4, COLS, WAVES, SC, DEPTH, DOWN>(a, expert, tile, pairs,
+                                                                                                       count, smem);
+        const int rows = count <= 16 ? 16 : 32;
+        __syncthreads();
+        auto total = [&](int row, int c) {
+            float4_t s = *reinterpret_cast<const float4_t *>(red + (size_t)row * COLS + c);
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w)
+                s += *reinterpret_cast<const float4_t *>(red + ((size_t)w * rows + row) * COLS + c);
+            return s;
+        };
+        if (!DOWN) {
+            for (int e = tid; e < count * (QUADS / 2); e += kThreads) {
+                const int row = e / (QUADS / 2), c = e % (QUADS / 2) * 4, n = tile * (COLS / 2) + c;
+                if (n >= N / 2)
+                    continue;
+                const float4_t gate = total(row, c), up = total(row, COLS / 2 + c);
+                half4_t h;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)  // rounded to fp16, as any activation between two products of this library
+                    h[j] = (half_t)(gate[j] / (1.f + __expf(-gate[j])) * up[j]);
+                *reinterpret_cast<half4_t *>(a.hidden + (size_t)pairs[row] * (N / 2) + n) = h;
+            }
+        } else {
+            for (int e = tid; e < count * QUADS; e += kThreads) {
+                const int row = e / QUADS, c = e % QUADS * 4, n = tile * COLS + c;
+                if (n >= N)
+                    continue;
+                const float4_t s = total(row, c);
+                unsigned long long *dst = reinterpret_cast<unsigned long long *>(a.partial + (size_t)pairs[row] * N + n);
+                __hip_atomic_store(dst, __builtin_bit_cast(unsigned long long, f32x2_t{s[0], s[1]}), __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(dst + 1, __builtin_bit_cast(unsigned long long, f32x2_t{s[2], s[3]}), __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+        done += count;
+    }
+    if (!DOWN)
+        return;
+    // The workgroup that brings the tile's pairs to the call's number adds every token's experts (exchange.h).
+    __builtin_amdgcn_s_waitcnt(0);  // every partial store of this workgroup has been acknowledged
+    __syncthreads();
+    if (tid == 0)
+        s_last = (int)slice_arrive(a.counters + tile, (unsigned)done) + done == total_pairs;
+    __syncthreads();
+    if (!s_last)
+        return;
+    slice_acquire();
+    for (int e = tid; e < a.M * QUADS; e += kThreads) {
+        const int m = e / QUADS, n = tile * COLS + e % QUADS * 4;
+        if (n >= N)
+            continue;
+        float4_t s = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < a.top_k; ++j) {
+            const int id = a.ids[m * a.top_k + j];
+            if (id < 0 || id >= a.experts)
+                continue;
+            const float w = a.weights[m * a.top_k + j];
+            const unsigned long long *src =
+                reinterpret_cast<const unsigned long long *>(a.partial + (size_t)(m * a.top_k + j) * N + n);
+            const f32x2_t lo = __builtin_bit_cast(f32x2_t, __hip_atomic_load(src, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            const f32x2_t hi =
+                __builtin_bit_cast(f32x2_t, __hip_atomic_load(src + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            s[0] = __builtin_fmaf(w, lo[0], s[0]);
+            s[1] = __builtin_fmaf(w, lo[1], s[1]);
+            s[2] = __builtin_fmaf(w, hi[0], s[2]);
+            s[3] = __builtin_fmaf(w, hi[1], s[3]);
+        }
+        *reinterpret_cast<half4_t *>(a.out + (size_t)m * N + n) =
+            half4_t{(half_t)s[0], (half_t)s[1], (half_t)s[2], (half_t)s[3]};
+    }
+    if (tid == 0)
+        __hip_atomic_store(a.counters + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+}  // namespace moe
+}  // namespace gptq

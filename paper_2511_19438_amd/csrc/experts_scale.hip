@@ -1,0 +1,55 @@
+// Instances of the experts' kernel for one kind of group size (GPTQ_EXPERTS_SCALING: 0 groups of 128 n, 1 of 64 n, 2 of 32 n)
+// and one of the two products (GPTQ_EXPERTS_DOWN).
+#include "experts_kernel.h"
+
+#if !defined(GPTQ_EXPERTS_SCALING) || !defined(GPTQ_EXPERTS_DOWN)
+#error "GPTQ_EXPERTS_SCALING and GPTQ_EXPERTS_DOWN must be defined"
+#endif
+
+namespace gptq {
+namespace moe {
+namespace {
+
+constexpr Scaling kScaling = (Scaling)GPTQ_EXPERTS_SCALING;
+
+constexpr bool kDown = GPTQ_EXPERTS_DOWN != 0;
+
+template <int ROWS, int COLS, int WAVES, int DEPTH>
+hipError_t launch_one(const Args &a, const Shape &s, hipStream_t stream)
+{
+    constexpr size_t lds = lds_bytes<(ROWS + 15) / 16, ROWS / 8, COLS, WAVES, kScaling, DEPTH>();
+    static_assert(lds <= 160 * 1024 - 64 - 4 * WAVES * ROWS, "one workgroup fits a compute unit");
+    auto kernel = experts_kernel<ROWS, COLS, WAVES, kScaling, DEPTH, kDown>;
+    if (lds > 48 * 1024) {
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (err != hipSuccess)
+            return err;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.tiles * s.groups), dim3(64 * WAVES), lds, stream, a);
+    return hipGetLastError();
+}
+
+template <int COLS, int WAVES, int DEPTH>
+hipError_t launch_rows(const Args &a, const Shape &s, hipStream_t stream)
+{
+    if (s.rows == 8)
+        return launch_one<8, COLS, WAVES, DEPTH>(a, s, stream);
+    if (s.rows == 16)
+        return launch_one<16, COLS, WAVES, DEPTH>(a, s, stream);
+    return launch_one<32, COLS, WAVES, DEPTH>(a, s, stream);
+}
+
+}  // namespace
+
+template <>
+hipError_t launch_product<GPTQ_EXPERTS_SCALING, kDown>(const Args &a, const Shape &s, hipStream_t stream)
+{
+    if constexpr (kDown)
+        return s.wide ? launch_rows<64, 4, 2>(a, s, stream) : launch_rows<32, 8, 3>(a, s, stream);
+    else
+        return s.wide ? launch_rows<128, 4, 2>(a, s, stream) : launch_rows<64, 4, 2>(a, s, stream);
+}
+
+}  // namespace moe
+}  // namespace gptq

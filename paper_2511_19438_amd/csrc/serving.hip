@@ -18,7 +18,7 @@ int check_route(int M, int experts, int top_k)
     return GPTQ_OK;
 }
 
-// Sizes of a layer of experts.  A column tile of the output has an arrival counter: 65536 of 64 columns each.
+// Sizes of a layer of experts.  A column tile of the output has an arrival counter: 65536 of 32 columns at least.
 int check_layer(int M, int hidden, int inter, int experts, int top_k, int group_size)
 {
     if (M <= 0 || hidden <= 0 || inter <= 0 || experts <= 0 || top_k <= 0 || group_size <= 0)
@@ -26,6 +26,9 @@ int check_layer(int M, int hidden, int inter, int experts, int top_k, int group_
     if (experts > moe::kMaxExperts || top_k > moe::kMaxTopK || (long long)M * top_k > moe::kMaxPairs)
         return GPTQ_UNSUPPORTED_SHAPE;
     if (group_size % 32 || hidden % group_size || inter % group_size || hidden > (1 << 20) || inter > (1 << 20))
+        return GPTQ_UNSUPPORTED_SHAPE;
+    // (32-bit byte offsets into the tokens and into the pairs' activations)
+    if ((long long)M * hidden >= (1ll << 31) || (long long)M * top_k * inter >= (1ll << 31))
         return GPTQ_UNSUPPORTED_SHAPE;
     const int rc = check_shape(hidden, 2 * inter, group_size);
     return rc != GPTQ_OK ? rc : check_shape(inter, hidden, group_size);
@@ -135,8 +138,8 @@ int gptq_w4a16_moe_experts(const void *x, const void *ids, const void *weights, 
     if (rc != GPTQ_OK)
         return rc;
     moe::Call c = make_call(x, experts, out, M, top_k);
-    c.ids = static_cast<const int32_t *>(ids);
-    c.weights = static_cast<const float *>(weights);
+    c.ids = const_cast<int32_t *>(static_cast<const int32_t *>(ids));  // (without logits nothing writes them)
+    c.weights = const_cast<float *>(static_cast<const float *>(weights));
     return status(moe::launch_experts(c, layout, scratch, counters, st));
 }
 
@@ -160,14 +163,13 @@ int gptq_w4a16_moe(const void *x, const void *logits, int logits_type, const gpt
     rc = layer_scratch(experts, M, top_k, st, layout, counters, scratch);
     if (rc != GPTQ_OK)
         return rc;
-    int32_t *ids = reinterpret_cast<int32_t *>(scratch + layout.ids);
-    float *weights = reinterpret_cast<float *>(scratch + layout.weights);
     moe::Call c = make_call(x, experts, out, M, top_k);
-    c.ids = ids;
-    c.weights = weights;
-    const hipError_t err = moe::launch_route(logits, logits_type == GPTQ_LOGITS_FP32, ids, weights, M, experts->experts,
-                                             top_k, renormalize != 0, st);
-    return status(err != hipSuccess ? err : moe::launch_experts(c, layout, scratch, counters, st));
+    c.ids = reinterpret_cast<int32_t *>(scratch + layout.ids);
+    c.weights = reinterpret_cast<float *>(scratch + layout.weights);
+    c.logits = logits;
+    c.logits_fp32 = logits_type == GPTQ_LOGITS_FP32;
+    c.renormalize = renormalize != 0;
+    return status(moe::launch_experts(c, layout, scratch, counters, st));
 }
 
 size_t gptq_w4a16_moe_workspace_bytes(int M, int hidden, int inter, int experts, int top_k, int group_size)
