@@ -84,8 +84,10 @@ GPTQ_API size_t gptq_w4a16_moe_workspace_bytes(int M, int hidden, int inter, int
  *     adapter  int32 [M]                     outside [0, adapters): the row has none, out[m] = base[m]
  *     base     fp16  [M, N], rows ld_base elements apart
  *     out      fp16  [M, N], rows ld_out elements apart; may be base itself (then ld_out == ld_base), no other overlap
- * x A^T and all sums are kept in fp32, the result is rounded once.  K, N, rank and the row strides are multiples of 8 with
- * ldx >= K, ld_base >= N, ld_out >= N; rank <= 256; adapters * rank * K and adapters * rank * N below 2^40.
+ * x A^T is summed and kept in fp32 (it enters the second product with 22 bits), all sums are fp32, the result is rounded
+ * once.  K, N, rank and the row strides are multiples of 8 with
+ * ldx >= K, ld_base >= N, ld_out >= N; rank <= 256; adapters * rank * K and adapters * rank * N below 2^40, M below 2^24,
+ * M * N below 2^33 (else GPTQ_UNSUPPORTED_SHAPE).
  */
 GPTQ_API int gptq_w4a16_lora_add(const void *x, const void *a, const void *b, const void *scaling, const void *adapter,
                                  const void *base, void *out, int M, int K, int N, int rank, int adapters, int ldx,

@@ -2,8 +2,13 @@
 //
 // Both kernels take tiles of 16 rows and go through the different adapters of a tile, so that an adapter is read once for
 // all of its rows there - a prompt's rows share one, a decode step's rows mostly have their own - and the host need not know
-// which rows have which.  A row takes its values from its own adapter's product by selection: whatever another adapter
-// holds, infinities included, does not reach it.
+// which rows have which.  An adapter's product is made for all 16 rows (the matrix instruction costs less than the adapter's
+// loads) and a row takes its values from its own adapter's by selection: whatever another adapter or another row holds,
+// infinities included, does not reach it.
+//
+// Both are bound by the latency of dependent loads - the row's adapter, then that adapter's data - and, in prompts, by
+// reading and writing the output.  So every wavefront asks for all it needs of several adapters, or for four steps of K, at
+// once.
 #include "adapters.h"
 
 namespace gptq {
@@ -21,167 +26,397 @@ struct Args {
     float *t;  // [slices, M, rank]
     half_t *out;
     long long ldx, ld_base, ld_out;
-    int M, K, N, rank, adapters, slices, slice_steps;
+    int M, K, N, rank, adapters, row_tiles, slots, slices, slice_steps, col_groups;
 };
 
-// The adapters of a tile's rows: lane i < 16 has that of row i, -1 for none; `first` marks the lanes whose adapter no row
-// before them has.
-struct TileAdapters {
-    int mine;
-    uint32_t first;
-    __device__ __forceinline__ TileAdapters(const Args &a, int m0, int lane)
-    {
-        mine = -1;
-        if (lane < kRows && m0 + lane < a.M)
-            mine = a.adapter[m0 + lane];
-        if (mine < 0 || mine >= a.adapters)
-            mine = -1;
-        bool before = false;
-#pragma unroll
-        for (int j = 0; j < kRows; ++j)
-            before |= j < lane && __builtin_amdgcn_readlane(mine, j) == mine;
-        first = (uint32_t)__ballot(mine >= 0 && !before);
-    }
-};
-
-constexpr int kRankTiles = 4;  // tiles of 16 ranks that are computed at a time
-
-__global__ __launch_bounds__(kThreads) void shrink_kernel(const Args a)
+// The adapters of a tile's rows: lane i < 16 has that of row i, -1 for none.
+__device__ __forceinline__ int adapter_of_row(const Args &a, int m0, int lane)
 {
-    __shared__ float red[kWaves][kRows][16 * kRankTiles];
+    int mine = -1;
+    if (lane < kRows && m0 + lane < a.M)
+        mine = a.adapter[m0 + lane];
+    return mine >= 0 && mine < a.adapters ? mine : -1;
+}
+
+// The first adapter among the rows `left` of a tile, all of whose rows leave the set.
+__device__ __forceinline__ int next_adapter(int mine, uint32_t &left)
+{
+    const int l = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
+    left &= ~(uint32_t)__ballot(mine == l);
+    return l;
+}
+
+__device__ __forceinline__ uint32_t rows_with_adapter(int mine)
+{
+    return (uint32_t)__ballot(mine >= 0);
+}
+
+// The products of a tile's rows with 16 * TILES ranks of adapter `la` from rank r0 on, over the steps s0 .. s1 of 32 k.
+template <int TILES, int BATCH>  // BATCH: steps that are loaded at a time
+__device__ __forceinline__ void project(const Args &a, const half_t *x, const half_t *la, int r0, int s0, int s1, int lane,
+                                        float4_t (&acc)[TILES])
+{
+    const int cq = lane & 15, kg = lane >> 4;
+    const half_t *arow[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+        acc[t] = float4_t{0.f, 0.f, 0.f, 0.f};
+        arow[t] = la + (size_t)min(r0 + 16 * t + cq, a.rank - 1) * a.K;  // (a rank past the last is not used)
+    }
+    for (int s = s0; s < s1; s += BATCH) {
+        half8_t xv[BATCH], av[BATCH][TILES];
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+            const int k = min((s + j) * 32 + kg * 8, a.K - 8);
+            xv[j] = *reinterpret_cast<const half8_t *>(x + k);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+                av[j][t] = *reinterpret_cast<const half8_t *>(arow[t] + k);
+        }
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+            const bool outside = s + j >= s1 || (s + j) * 32 + kg * 8 >= a.K;  // loaded a second time: zeros on both sides
+            if (outside)
+                xv[j] = half8_t{};
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                if (outside)
+                    av[j][t] = half8_t{};
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[j], av[j][t], acc[t], 0, 0, 0);
+            }
+        }
+    }
+}
+
+// ---- shrink: a workgroup has 16 rows, a slice of K and 16 * TILES ranks of some of the tile's adapters; its wavefronts
+//      split the slice, their sums meet in LDS, those of the slices in the expand kernel ----
+template <int TILES, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void shrink_kernel(const Args a)
+{
+    __shared__ float red[WAVES][kRows][16 * TILES];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int cq = lane & 15, kg = lane >> 4;
     const int m0 = blockIdx.x * kRows;
-    const TileAdapters rows(a, m0, lane);
+    const int r0 = (blockIdx.z / a.slots) * 16 * TILES, slot = blockIdx.z % a.slots;
+    const int mine = adapter_of_row(a, m0, lane);
     const int steps = (a.K + 31) / 32;
     const int b0 = blockIdx.y * a.slice_steps, b1 = min(b0 + a.slice_steps, steps);
-    const int per_wave = (b1 - b0 + kWaves - 1) / kWaves;
+    const int per_wave = (b1 - b0 + WAVES - 1) / WAVES;
     const int s0 = min(b0 + wave * per_wave, b1), s1 = min(s0 + per_wave, b1);
     const half_t *x = a.x + min(m0 + cq, a.M - 1) * a.ldx;
     int index = 0;
-    for (uint32_t left = rows.first; left != 0; left &= left - 1, ++index) {
-        if (index % gridDim.z != blockIdx.z)
+    for (uint32_t left = rows_with_adapter(mine); left != 0; ++index) {
+        const int l = next_adapter(mine, left);
+        if (index % a.slots != slot)
             continue;
-        const int l = __builtin_amdgcn_readlane(rows.mine, __builtin_ctz(left));
-        const half_t *la = a.a + (size_t)l * a.rank * a.K;
-        for (int r0 = 0; r0 < a.rank; r0 += 16 * kRankTiles) {
-            float4_t acc[kRankTiles];
-            const half_t *arow[kRankTiles];
+        float4_t acc[TILES];
+        project<TILES, 4>(a, x, a.a + (size_t)l * a.rank * a.K, r0, s0, s1, lane, acc);
+        __syncthreads();  // (the sums of the adapter before have been read)
 #pragma unroll
-            for (int t = 0; t < kRankTiles; ++t) {
-                acc[t] = float4_t{0.f, 0.f, 0.f, 0.f};
-                arow[t] = la + (size_t)min(r0 + 16 * t + cq, a.rank - 1) * a.K;
-            }
-            for (int s = s0; s < s1; ++s) {
-                const int k = s * 32 + kg * 8;
-                half8_t xv = {}, av[kRankTiles] = {};
-                if (k < a.K) {
-                    xv = *reinterpret_cast<const half8_t *>(x + k);
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                    for (int t = 0; t < kRankTiles; ++t)
-                        if (r0 + 16 * t < a.rank)
-                            av[t] = *reinterpret_cast<const half8_t *>(arow[t] + k);
-                }
+            for (int r = 0; r < 4; ++r)
+                red[wave][4 * kg + r][16 * t + cq] = acc[t][r];
+        __syncthreads();
+        for (int e = tid; e < kRows * 16 * TILES; e += 64 * WAVES) {
+            const int row = e / (16 * TILES), c = e % (16 * TILES);
+            const int owner = __shfl(mine, row);  // (whole wavefronts come here)
+            if (owner != l || r0 + c >= a.rank)
+                continue;
+            float sum = red[0][row][c];
 #pragma unroll
-                for (int t = 0; t < kRankTiles; ++t)
-                    if (r0 + 16 * t < a.rank)
-                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, av[t], acc[t], 0, 0, 0);
-            }
-            __syncthreads();  // (the sums of the adapter or ranks before have been read)
-#pragma unroll
-            for (int t = 0; t < kRankTiles; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    red[wave][4 * kg + r][16 * t + cq] = acc[t][r];
-            __syncthreads();
-            for (int e = tid; e < kRows * 16 * kRankTiles; e += kThreads) {
-                const int row = e / (16 * kRankTiles), c = e % (16 * kRankTiles);
-                const int owner = __shfl(rows.mine, row);  // (a wavefront's 64 elements are one row: all lanes take part)
-                if (owner != l || r0 + c >= a.rank)
-                    continue;
-                float sum = red[0][row][c];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w)
-                    sum += red[w][row][c];
-                a.t[((size_t)blockIdx.y * a.M + m0 + row) * a.rank + r0 + c] = sum;
-            }
+            for (int w = 1; w < WAVES; ++w)
+                sum += red[w][row][c];
+            a.t[((size_t)blockIdx.y * a.M + m0 + row) * a.rank + r0 + c] = sum;
         }
     }
 }
 
-constexpr int kCols = 16 * kWaves;
-
-__global__ __launch_bounds__(kThreads) void expand_kernel(const Args a)
+// t of a row: the sums of the slices, in their order, eight of them loaded at a time.
+__device__ __forceinline__ float sum_of_slices(const Args &a, int m, int r)
 {
-    __shared__ __align__(16) float ts[kRows][kMaxRank + 4];
+    const float *src = a.t + (size_t)m * a.rank + r;
+    const size_t step = (size_t)a.M * a.rank;
+    float sum = 0.f;
+    for (int i0 = 0; i0 < a.slices; i0 += 8) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = src[min(i0 + i, a.slices - 1) * step];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            sum += i0 + i < a.slices ? v[i] : 0.f;
+    }
+    return sum;
+}
+
+// ---- expand, few rows: a workgroup has one row and 256 * COLS columns, all in fp32.  (The matrix instruction multiplies 16
+//      rows where one is wanted, after a longer way through LDS: 32 rows of 12288 columns 7.9 us, here 4.0.) ----
+template <int COLS, int PIECES>  // PIECES: of 8 ranks that are loaded at a time
+__global__ __launch_bounds__(kThreads) void expand_row_kernel(const Args a)
+{
+    typedef half_t vec __attribute__((ext_vector_type(COLS)));
+    __shared__ __align__(16) float t[kMaxRank];
+    const int m = blockIdx.x % a.M;
+    const int n = (blockIdx.x / a.M * kThreads + threadIdx.x) * COLS;
+    const int nc = min(n, a.N - COLS);
+    const int l = __builtin_amdgcn_readfirstlane(a.adapter[m]);
+    const bool bare = l < 0 || l >= a.adapters;
+    if (bare && a.base == a.out)
+        return;
+    const vec base = *reinterpret_cast<const vec *>(a.base + m * a.ld_base + nc);
+    vec out = base;
+    if (!bare) {
+        const float scaling = a.scaling[l];
+        const half_t *lb = a.b + ((size_t)l * a.N + nc) * a.rank;
+        half8_t b[COLS][PIECES];
+        auto load = [&](int r0) {
+#pragma unroll
+            for (int c = 0; c < COLS; ++c)
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p)  // (a piece past the last: the last again, not used)
+                    b[c][p] = *reinterpret_cast<const half8_t *>(lb + c * a.rank + min(r0 + 8 * p, a.rank - 8));
+        };
+        load(0);
+        if ((int)threadIdx.x < kMaxRank) {
+            t[threadIdx.x] = (int)threadIdx.x < a.rank ? sum_of_slices(a, m, threadIdx.x) : 0.f;
+        }
+        __syncthreads();
+        float sum[COLS] = {};
+        for (int r0 = 0;;) {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                float tv[8];
+                *reinterpret_cast<float4_t *>(tv) = *reinterpret_cast<const float4_t *>(t + r0 + 8 * p);
+                *reinterpret_cast<float4_t *>(tv + 4) = *reinterpret_cast<const float4_t *>(t + r0 + 8 * p + 4);
+                const bool inside = r0 + 8 * p < a.rank;
+#pragma unroll
+                for (int c = 0; c < COLS; ++c) {
+                    float part = sum[c];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        part = __builtin_fmaf(tv[k], (float)b[c][p][k], part);
+                    sum[c] = inside ? part : sum[c];
+                }
+            }
+            r0 += 8 * PIECES;
+            if (r0 >= a.rank)
+                break;
+            load(r0);
+        }
+#pragma unroll
+        for (int c = 0; c < COLS; ++c)
+            out[c] = (half_t)__builtin_fmaf(scaling, sum[c], (float)base[c]);
+    }
+    if (n < a.N)
+        *reinterpret_cast<vec *>(a.out + m * a.ld_out + n) = out;
+}
+
+// t of 16 rows as the operand of the second product.  t is kept in fp32 up to here.  The matrix instruction takes fp16, so t
+// goes in as the sum of two fp16 numbers, after a power of two has brought the row's largest to [1, 2): what is lost is 2^-22
+// of that largest, as if t had been rounded to 22 bits (the fp32 instruction takes eight times as long).
+template <int CHUNKS>  // of 32 ranks
+struct Operand {
+    static constexpr int RANKS = 32 * CHUNKS;
+    half_t hi[kRows][RANKS + 8], lo[kRows][RANKS + 8];
+    float factor[kRows];  // scaling and that power of two
+
+    // By 16 threads a row: `part` of them, with t of the ranks part + 16 j; l: the row's adapter.
+    __device__ __forceinline__ void put(const Args &a, int row, int part, int l, const float (&t)[RANKS / 16])
+    {
+        uint32_t largest = 0;
+#pragma unroll
+        for (int j = 0; j < RANKS / 16; ++j) {
+            const uint32_t bits = __builtin_bit_cast(uint32_t, t[j]) & 0x7fffffffu;
+            largest = bits > largest ? bits : largest;
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+            const uint32_t other = __shfl_xor(largest, d);
+            largest = other > largest ? other : largest;
+        }
+        const int exponent = (int)(largest >> 23);  // (infinities and NaN go through as they are)
+        const int shift = exponent == 255 || largest == 0 ? 0 : exponent - 127;
+#pragma unroll
+        for (int j = 0; j < RANKS / 16; ++j) {
+            const float v = ldexpf(t[j], -shift);
+            const half_t h = (half_t)v;
+            hi[row][part + 16 * j] = h;
+            lo[row][part + 16 * j] = exponent == 255 ? (half_t)0.f : (half_t)(v - (float)h);
+        }
+        if (part == 0)
+            factor[row] = l >= 0 ? ldexpf(a.scaling[l], shift) : 0.f;
+    }
+};
+
+// ---- expand, many rows: a workgroup has 16 rows and 256 columns at a time, a wavefront 64 of them, a lane four that stand
+//      together.  Workgroups that follow each other have other columns, so that the columns of a workgroup's XCD are mostly
+//      the same and its L2 keeps their B ----
+template <int CHUNKS>
+__global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(const Args a)
+{
+    constexpr int PER = 2 * CHUNKS;  // ranks of a row that a thread brings to LDS
+    constexpr int TILES = 4;
+    __shared__ __align__(16) Operand<CHUNKS> operand;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int cq = lane & 15, kg = lane >> 4;
-    const int m0 = blockIdx.y * kRows;
-    const TileAdapters rows(a, m0, lane);
-    const int padded = (a.rank + 31) & ~31;
-    for (int row = wave; row < kRows; row += kWaves) {
-        const int l = __builtin_amdgcn_readlane(rows.mine, row);
-        const float s = l >= 0 ? a.scaling[l] : 0.f;
-        for (int r = lane; r < padded; r += 64) {
-            float sum = 0.f;
-            if (l >= 0 && r < a.rank)
-                for (int i = 0; i < a.slices; ++i)
-                    sum += a.t[((size_t)i * a.M + m0 + row) * a.rank + r];
-            ts[row][r] = s * sum;
-        }
-    }
-    __syncthreads();
-    const int n = blockIdx.x * kCols + wave * 16 + cq;
-    const int nc = min(n, a.N - 1);
-    float4_t acc = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t left = rows.first; left != 0; left &= left - 1) {
-        const int l = __builtin_amdgcn_readlane(rows.mine, __builtin_ctz(left));
-        const half_t *lb = a.b + ((size_t)l * a.N + nc) * a.rank;
-        float4_t d = {0.f, 0.f, 0.f, 0.f};
-        for (int r0 = 0; r0 < a.rank; r0 += 32) {
-            const int r = r0 + kg * 8;
-            half8_t bv = {};
-            if (r < a.rank)
-                bv = *reinterpret_cast<const half8_t *>(lb + r);
+    const int m0 = blockIdx.x / a.col_groups * kRows, m = m0 + 4 * kg;
+    const int mine = adapter_of_row(a, m0, lane);
+    const uint32_t all = rows_with_adapter(mine);
+    if (all == 0 && a.base == a.out)
+        return;
+
+    half8_t bv[TILES][CHUNKS];
+    half4_t base[4];
+    int n;
+    auto load_adapter = [&](int l) {
+        const half_t *lb = a.b + ((size_t)l * a.N + min(n, a.N - TILES)) * a.rank;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                d = __builtin_amdgcn_mfma_f32_16x16x4f32(ts[cq][r + j], (float)bv[j], d, 0, 0, 0);
-        }
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {  // (ranks past the last: zeros)
+                const int r = 32 * c + kg * 8;
+                const half8_t v = *reinterpret_cast<const half8_t *>(lb + t * a.rank + min(r, a.rank - 8));
+                bv[t][c] = r < a.rank ? v : half8_t{};
+            }
+    };
+    auto begin = [&](int tile, uint32_t &left) {  // loads of the tile's outputs and of its first adapter
+        n = (tile * kWaves + wave) * 16 * TILES + TILES * cq;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            acc[r] = __shfl(rows.mine, 4 * kg + r) == l ? d[r] : acc[r];
+            base[r] = *reinterpret_cast<const half4_t *>(a.base + min(m + r, a.M - 1) * a.ld_base + min(n, a.N - TILES));
+        const int l = left ? next_adapter(mine, left) : -1;
+        if (l >= 0)
+            load_adapter(l);
+        return l;
+    };
+    int tile = blockIdx.x % a.col_groups;
+    uint32_t left = all;
+    int l = begin(tile, left);
+    {
+        const int row = tid >> 4, part = tid & 15;
+        const int own = __shfl(mine, row);
+        float sum[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int r = part + 16 * j;
+            sum[j] = own >= 0 && r < a.rank ? sum_of_slices(a, m0 + row, r) : 0.f;
+        }
+        operand.put(a, row, part, own, sum);
     }
+    __syncthreads();
+    half8_t hi[CHUNKS], lo[CHUNKS];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        hi[c] = *reinterpret_cast<const half8_t *>(&operand.hi[cq][32 * c + kg * 8]);
+        lo[c] = *reinterpret_cast<const half8_t *>(&operand.lo[cq][32 * c + kg * 8]);
+    }
+    int owner[4];
+    float factor[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int row = 4 * kg + r, m = m0 + row;
-        const bool bare = __shfl(rows.mine, row) < 0;
-        if (m >= a.M || n >= a.N)
-            continue;
-        const half_t base = a.base[m * a.ld_base + n];
-        a.out[m * a.ld_out + n] = bare ? base : (half_t)((float)base + acc[r]);
+        owner[r] = __shfl(mine, 4 * kg + r);
+        factor[r] = operand.factor[4 * kg + r];
+    }
+    for (;;) {
+        float4_t acc[TILES];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+            acc[t] = float4_t{0.f, 0.f, 0.f, 0.f};
+        while (l >= 0) {
+            const bool chosen[4] = {owner[0] == l, owner[1] == l, owner[2] == l, owner[3] == l};
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                float4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[c], bv[t][c], d, 0, 0, 0);
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[c], bv[t][c], d, 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    acc[t][r] = chosen[r] ? d[r] : acc[t][r];
+            }
+            l = -1;
+            if (left) {
+                l = next_adapter(mine, left);
+                load_adapter(l);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            half4_t out;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const half_t sum = (half_t)__builtin_fmaf(factor[r], acc[t][r], (float)base[r][t]);
+                out[t] = owner[r] < 0 ? base[r][t] : sum;
+            }
+            if (n < a.N && m + r < a.M)
+                *reinterpret_cast<half4_t *>(a.out + (m + r) * a.ld_out + n) = out;
+        }
+        tile += a.col_groups;
+        if (tile * 256 >= a.N)
+            break;
+        left = all;
+        l = begin(tile, left);
     }
 }
+
+constexpr int kFewRows = 64;
 
 int row_tiles(int M)
 {
     return (M + kRows - 1) / kRows;
 }
 
-// Workgroups along the adapters of a tile: a decode step's rows mostly have their own each.
+// Workgroups along the adapters of a tile.  A decode step's rows mostly have their own each, a prompt's few.
 int adapter_slots(int M)
 {
-    return M <= 64 ? (M < kRows ? M : kRows) : 2;
+    return M < kRows ? M : M <= kFewRows ? kRows : 4;
 }
 
+// Slices of K: 512 k each, which a workgroup loads at once, while the workgroups are no more than twice the compute units.
 int k_slices(int M, int K)
 {
-    const int groups = row_tiles(M) * adapter_slots(M);
-    int slices = 256 / groups;
-    const int most = (K + 511) / 512;
-    slices = slices > most ? most : slices;
-    return slices < 1 ? 1 : slices;
+    const int most = (K + 511) / 512, slices = 512 / (row_tiles(M) * adapter_slots(M));
+    return slices < 1 ? 1 : slices > most ? most : slices;
+}
+
+template <int TILES, int WAVES>
+void launch_shrink(const Args &a, hipStream_t stream)
+{
+    const int chunks = (a.rank + 16 * TILES - 1) / (16 * TILES);
+    shrink_kernel<TILES, WAVES><<<dim3(a.row_tiles, a.slices, a.slots * chunks), 64 * WAVES, 0, stream>>>(a);
+}
+
+template <int COLS>
+void launch_expand_rows(const Args &a, hipStream_t stream)
+{
+    const int cols = COLS * kThreads;
+    const dim3 grid((unsigned)((a.N + cols - 1) / cols) * a.M);
+    if (a.rank <= 8)
+        expand_row_kernel<COLS, 1><<<grid, kThreads, 0, stream>>>(a);
+    else if (a.rank <= 16)
+        expand_row_kernel<COLS, 2><<<grid, kThreads, 0, stream>>>(a);
+    else if (a.rank <= 32)
+        expand_row_kernel<COLS, 4><<<grid, kThreads, 0, stream>>>(a);
+    else
+        expand_row_kernel<COLS, 8><<<grid, kThreads, 0, stream>>>(a);
+}
+
+void launch_expand(const Args &a, hipStream_t stream)
+{
+    const dim3 grid((unsigned)a.row_tiles * a.col_groups);
+    if (a.rank <= 32)
+        expand_kernel<1><<<grid, kThreads, 0, stream>>>(a);
+    else if (a.rank <= 64)
+        expand_kernel<2><<<grid, kThreads, 0, stream>>>(a);
+    else if (a.rank <= 128)
+        expand_kernel<4><<<grid, kThreads, 0, stream>>>(a);
+    else
+        expand_kernel<8><<<grid, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -210,11 +445,21 @@ hipError_t launch_lora(const Call &c, void *scratch, hipStream_t stream)
     a.N = c.N;
     a.rank = c.rank;
     a.adapters = c.adapters;
+    a.row_tiles = row_tiles(c.M);
+    a.slots = c.adapters < adapter_slots(c.M) ? c.adapters : adapter_slots(c.M);
     const int steps = (c.K + 31) / 32;
     a.slices = k_slices(c.M, c.K);
     a.slice_steps = (steps + a.slices - 1) / a.slices;
-    shrink_kernel<<<dim3(row_tiles(c.M), a.slices, adapter_slots(c.M)), kThreads, 0, stream>>>(a);
-    expand_kernel<<<dim3((c.N + kCols - 1) / kCols, row_tiles(c.M)), kThreads, 0, stream>>>(a);
+    if (c.M <= kFewRows) {
+        launch_shrink<1, 4>(a, stream);
+        launch_expand_rows<1>(a, stream);
+    } else {
+        // one turn of 256 columns to a workgroup until there are eight workgroups to a compute unit
+        const int tiles = (c.N + 255) / 256, turns = (int)(((long long)tiles * a.row_tiles + 2047) / 2048);
+        a.col_groups = (tiles + turns - 1) / turns;
+        launch_shrink<2, 4>(a, stream);
+        launch_expand(a, stream);
+    }
     return hipGetLastError();
 }
 

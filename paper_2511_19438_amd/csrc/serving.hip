@@ -88,7 +88,8 @@ int check_lora(const void *x, const void *a, const void *b, const void *scaling,
         ldx < K || ld_base < N || ld_out < N || (base == out && ld_base != ld_out))
         return GPTQ_INVALID_ARG;
     if (K % 8 || N % 8 || rank % 8 || ldx % 8 || ld_base % 8 || ld_out % 8 || rank > lora::kMaxRank || K >= (1 << 23) ||
-        N >= (1 << 24) || (long long)adapters * rank * K >= (1ll << 40) || (long long)adapters * rank * N >= (1ll << 40))
+        N >= (1 << 24) || (long long)adapters * rank * K >= (1ll << 40) || (long long)adapters * rank * N >= (1ll << 40) ||
+        M >= (1 << 24) || (long long)M * N >= (1ll << 33))  // (workgroups of a launch)
         return GPTQ_UNSUPPORTED_SHAPE;
     if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(scaling) || !aligned16(adapter) || !aligned16(base) ||
         !aligned16(out))
