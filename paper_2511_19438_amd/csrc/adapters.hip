@@ -133,19 +133,20 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(const Args a)
     }
 }
 
-// t of a row: the sums of the slices, in their order, eight of them loaded at a time.
+// t of a row: the sums of the slices, in their order, BATCH of them loaded at a time.
+template <int BATCH>
 __device__ __forceinline__ float sum_of_slices(const Args &a, int m, int r)
 {
     const float *src = a.t + (size_t)m * a.rank + r;
     const size_t step = (size_t)a.M * a.rank;
     float sum = 0.f;
-    for (int i0 = 0; i0 < a.slices; i0 += 8) {
-        float v[8];
+    for (int i0 = 0; i0 < a.slices; i0 += BATCH) {
+        float v[BATCH];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < BATCH; ++i)
             v[i] = src[min(i0 + i, a.slices - 1) * step];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < BATCH; ++i)
             sum += i0 + i < a.slices ? v[i] : 0.f;
     }
     return sum;
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void expand_row_kernel(const Args a)
         };
         load(0);
         if ((int)threadIdx.x < kMaxRank) {
-            t[threadIdx.x] = (int)threadIdx.x < a.rank ? sum_of_slices(a, m, threadIdx.x) : 0.f;
+            t[threadIdx.x] = (int)threadIdx.x < a.rank ? sum_of_slices<8>(a, m, threadIdx.x) : 0.f;
         }
         __syncthreads();
         float sum[COLS] = {};
@@ -250,9 +251,10 @@ struct Operand {
     }
 };
 
-// ---- expand, many rows: a workgroup has 16 rows and 256 columns at a time, a wavefront 64 of them, a lane four that stand
-//      together.  Workgroups that follow each other have other columns, so that the columns of a workgroup's XCD are mostly
-//      the same and its L2 keeps their B ----
+// ---- expand, many rows: a workgroup has 16 rows and 256 columns at a time, a wavefront 64 of them.  B is the first operand of
+//      the matrix instruction and t the second, so that a lane has one row and, with the columns dealt out to the operand's
+//      rows in fours, 16 columns that stand together: full lines on both sides.  (The other way round, a lane with four rows
+//      of four columns: 512 rows of 12288 columns at rank 32 14.2 us, here 12.3.) ----
 template <int CHUNKS>
 __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(const Args a)
 {
@@ -262,34 +264,38 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int cq = lane & 15, kg = lane >> 4;
-    const int m0 = blockIdx.x / a.col_groups * kRows, m = m0 + 4 * kg;
+    const int m0 = blockIdx.x / a.col_groups * kRows, m = m0 + cq;
     const int mine = adapter_of_row(a, m0, lane);
     const uint32_t all = rows_with_adapter(mine);
     if (all == 0 && a.base == a.out)
         return;
+    const int owner = __shfl(mine, cq);
 
     half8_t bv[TILES][CHUNKS];
-    half4_t base[4];
-    int n;
+    half8_t base[2];
+    int n0;
     auto load_adapter = [&](int l) {
-        const half_t *lb = a.b + ((size_t)l * a.N + min(n, a.N - TILES)) * a.rank;
+        const half_t *lb = a.b + (size_t)l * a.N * a.rank;
 #pragma unroll
-        for (int t = 0; t < TILES; ++t)
+        for (int t = 0; t < TILES; ++t) {
+            const half_t *row = lb + (size_t)min(n0 + 16 * (cq >> 2) + 4 * t + (cq & 3), a.N - 1) * a.rank;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {  // (ranks past the last: zeros)
                 const int r = 32 * c + kg * 8;
-                const half8_t v = *reinterpret_cast<const half8_t *>(lb + t * a.rank + min(r, a.rank - 8));
+                const half8_t v = *reinterpret_cast<const half8_t *>(row + min(r, a.rank - 8));
                 bv[t][c] = r < a.rank ? v : half8_t{};
             }
+        }
     };
+    const half_t *const base_row = a.base + min(m, a.M - 1) * a.ld_base;
     auto begin = [&](int tile, uint32_t &left) {  // loads of the tile's outputs and of its first adapter
-        n = (tile * kWaves + wave) * 16 * TILES + TILES * cq;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            base[r] = *reinterpret_cast<const half4_t *>(a.base + min(m + r, a.M - 1) * a.ld_base + min(n, a.N - TILES));
+        n0 = (tile * kWaves + wave) * 16 * TILES;
         const int l = left ? next_adapter(mine, left) : -1;
         if (l >= 0)
             load_adapter(l);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            base[h] = *reinterpret_cast<const half8_t *>(base_row + min(n0 + 16 * kg + 8 * h, a.N - 8));
         return l;
     };
     int tile = blockIdx.x % a.col_groups;
@@ -302,7 +308,7 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int r = part + 16 * j;
-            sum[j] = own >= 0 && r < a.rank ? sum_of_slices(a, m0 + row, r) : 0.f;
+            sum[j] = own >= 0 && r < a.rank ? sum_of_slices<4>(a, m0 + row, r) : 0.f;
         }
         operand.put(a, row, part, own, sum);
     }
@@ -313,31 +319,25 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
         hi[c] = *reinterpret_cast<const half8_t *>(&operand.hi[cq][32 * c + kg * 8]);
         lo[c] = *reinterpret_cast<const half8_t *>(&operand.lo[cq][32 * c + kg * 8]);
     }
-    int owner[4];
-    float factor[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        owner[r] = __shfl(mine, 4 * kg + r);
-        factor[r] = operand.factor[4 * kg + r];
-    }
+    const float factor = operand.factor[cq];
     for (;;) {
         float4_t acc[TILES];
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
             acc[t] = float4_t{0.f, 0.f, 0.f, 0.f};
         while (l >= 0) {
-            const bool chosen[4] = {owner[0] == l, owner[1] == l, owner[2] == l, owner[3] == l};
+            const bool chosen = owner == l;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 float4_t d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
-                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[c], bv[t][c], d, 0, 0, 0);
-                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[c], bv[t][c], d, 0, 0, 0);
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[t][c], lo[c], d, 0, 0, 0);
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[t][c], hi[c], d, 0, 0, 0);
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    acc[t][r] = chosen[r] ? d[r] : acc[t][r];
+                    acc[t][r] = chosen ? d[r] : acc[t][r];
             }
             l = -1;
             if (left) {
@@ -346,15 +346,16 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
             }
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            half4_t out;
+        for (int h = 0; h < 2; ++h) {
+            half8_t out;
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                const half_t sum = (half_t)__builtin_fmaf(factor[r], acc[t][r], (float)base[r][t]);
-                out[t] = owner[r] < 0 ? base[r][t] : sum;
+            for (int j = 0; j < 8; ++j) {
+                const half_t sum = (half_t)__builtin_fmaf(factor, acc[2 * h + j / 4][j % 4], (float)base[h][j]);
+                out[j] = owner < 0 ? base[h][j] : sum;
             }
-            if (n < a.N && m + r < a.M)
-                *reinterpret_cast<half4_t *>(a.out + (m + r) * a.ld_out + n) = out;
+            const int n = n0 + 16 * kg + 8 * h;
+            if (n < a.N && m < a.M)
+                *reinterpret_cast<half8_t *>(a.out + m * a.ld_out + n) = out;
         }
         tile += a.col_groups;
         if (tile * 256 >= a.N)
