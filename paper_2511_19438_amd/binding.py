@@ -22,6 +22,7 @@ LIB_PATH = os.path.join(_HERE, "lib", "libgptq_w4a16.so")
 
 _lib = None
 _native_gemm = None  # csrc/native_call.cpp: tensors to the C ABI in one call; None before load() and where there is none
+_native_module = None  # the module that has it
 _addresses = {}      # of the entry points that it calls
 
 
@@ -96,16 +97,19 @@ def load() -> ctypes.CDLL:
 
 def _load_native_call(path):
     """gemm() of the extension module at `path`; None if it was not built for this torch and Python or cannot be loaded, and
-    calls are marshalled below."""
+    calls are marshalled below.  The module itself is kept in _native_module (serving.py calls its other functions)."""
+    global _native_module
+    _native_module = None
     if not os.path.exists(path):
         return None
     try:
         spec = importlib.util.spec_from_file_location("_native_call", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-        return module.gemm
     except (ImportError, OSError):
         return None
+    _native_module = module
+    return module.gemm
 
 
 def strerror(code: int) -> str:

@@ -94,6 +94,7 @@ def build_native_call():
         torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
         cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+               "-I", os.path.join(ROOT, "include"),
                "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(rocm, "include")]
         for include in cpp_extension.include_paths():
             cmd += ["-isystem", include]

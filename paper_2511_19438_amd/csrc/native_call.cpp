@@ -1,4 +1,4 @@
-// CPython extension module `_native_call`: the marshalling of a GEMM call from tensors to the C ABI.
+// CPython extension module `_native_call`: the marshalling of a call from tensors to the C ABI.
 //
 // A single-row product takes about 5 us on the GPU and 2.9 us of library and launch on the host; checking and unpacking
 // six tensors in Python and the foreign-function call took another 2.9 us, so that a stream of small calls was bound by
@@ -10,9 +10,13 @@
 
 #include <limits.h>
 
+#include <initializer_list>
+
 #include <ATen/core/Tensor.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include "gptq_w4a16_serving.h"
 
 namespace {
 
@@ -69,9 +73,283 @@ PyObject *gemm(PyObject *, PyObject *const *args, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
+// ---- the operators of gptq_w4a16_serving.h; the first argument is the function's address everywhere ----
+
+template <typename FN>
+FN address(PyObject *obj)
+{
+    void *p = PyLong_CheckExact(obj) ? PyLong_AsVoidPtr(obj) : nullptr;
+    if (PyErr_Occurred())
+        PyErr_Clear();
+    return reinterpret_cast<FN>(p);
+}
+
+// A plain integer that an int can hold; false for anything else.
+bool integer(PyObject *obj, int &value)
+{
+    if (!PyLong_CheckExact(obj))
+        return false;
+    const long v = PyLong_AsLong(obj);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    value = (int)v;
+    return v >= INT_MIN && v <= INT_MAX;
+}
+
+bool truth(PyObject *obj, int &value)
+{
+    value = obj == Py_True;
+    return obj == Py_True || obj == Py_False;
+}
+
+bool sizes(const at::Tensor *t, std::initializer_list<int64_t> want)
+{
+    if (!t || t->dim() != (int64_t)want.size())
+        return false;
+    int64_t i = 0;
+    for (int64_t w : want)
+        if (t->size(i++) != w)
+            return false;
+    return true;
+}
+
+bool fit(std::initializer_list<int64_t> values)
+{
+    for (int64_t v : values)
+        if (v > INT_MAX)
+            return false;
+    return true;
+}
+
+const at::Tensor *logits_of(PyObject *obj, int &type)
+{
+    const at::Tensor *t = plain(obj, at::kHalf, 2);
+    type = t ? GPTQ_LOGITS_FP16 : GPTQ_LOGITS_FP32;
+    return t ? t : plain(obj, at::kFloat, 2);
+}
+
+// (qweight, qzeros, scales) of `experts` matrices [K, N].
+bool matrices(PyObject *obj, int64_t experts, int64_t K, int64_t N, int group, const void *(&out)[3])
+{
+    if (!PyTuple_CheckExact(obj) || PyTuple_GET_SIZE(obj) != 3 || group <= 0 || K % group || K % 8 || N % 8)
+        return false;
+    const at::Tensor *w = plain(PyTuple_GET_ITEM(obj, 0), at::kInt, 3), *z = plain(PyTuple_GET_ITEM(obj, 1), at::kInt, 3);
+    const at::Tensor *s = plain(PyTuple_GET_ITEM(obj, 2), at::kHalf, 3);
+    if (!sizes(w, {experts, K / 8, N}) || !sizes(z, {experts, K / group, N / 8}) || !sizes(s, {experts, K / group, N}))
+        return false;
+    out[0] = w->data_ptr();
+    out[1] = z->data_ptr();
+    out[2] = s->data_ptr();
+    return true;
+}
+
+// The layer that x [M, hidden], gate_up, down and out describe.
+bool layer(const at::Tensor *x, PyObject *gate_up, PyObject *down, const at::Tensor *out, int group, gptq_w4a16_experts_t &e)
+{
+    if (!x || !PyTuple_CheckExact(gate_up) || PyTuple_GET_SIZE(gate_up) != 3)
+        return false;
+    const at::Tensor *w = plain(PyTuple_GET_ITEM(gate_up, 0), at::kInt, 3);
+    if (!w || w->size(2) % 2)
+        return false;
+    const int64_t M = x->size(0), hidden = x->size(1), experts = w->size(0), inter = w->size(2) / 2;
+    const void *g[3], *d[3];
+    if (!fit({M, hidden, 2 * inter, experts}) || !sizes(out, {M, hidden}) || !matrices(gate_up, experts, hidden, 2 * inter, group, g) ||
+        !matrices(down, experts, inter, hidden, group, d))
+        return false;
+    e = {g[0], g[1], g[2], d[0], d[1], d[2], (int)experts, (int)hidden, (int)inter, group};
+    return true;
+}
+
+// A matrix whose rows may stand apart, and their distance.
+const at::Tensor *strided(PyObject *obj, int64_t &ld)
+{
+    if (!THPVariable_CheckExact(obj))
+        return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(obj);
+    if (!t.defined() || !t.is_cuda() || t.scalar_type() != at::kHalf || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1))
+        return nullptr;
+    ld = t.size(0) > 1 ? t.stride(0) : t.size(1);
+    return ld >= t.size(1) && ld <= INT_MAX ? &t : nullptr;
+}
+
+struct Adapters {
+    const void *a, *b, *scaling, *adapter;
+    int M, K, N, rank, count;
+};
+
+bool adapters(const at::Tensor *x, PyObject *const *args, const at::Tensor *out, Adapters &l)
+{
+    const at::Tensor *a = plain(args[0], at::kHalf, 3), *b = plain(args[1], at::kHalf, 3);
+    const at::Tensor *scaling = plain(args[2], at::kFloat, 1), *adapter = plain(args[3], at::kInt, 1);
+    if (!x || !a || !out)
+        return false;
+    const int64_t M = x->size(0), K = x->size(1), N = out->size(1), count = a->size(0), rank = a->size(1);
+    if (!fit({M, K, N, count, rank}) || !sizes(a, {count, rank, K}) || !sizes(b, {count, N, rank}) || !sizes(scaling, {count}) ||
+        !sizes(adapter, {M}) || !sizes(out, {M, N}))
+        return false;
+    l = {a->data_ptr(), b->data_ptr(), scaling->data_ptr(), adapter->data_ptr(), (int)M, (int)K, (int)N, (int)rank, (int)count};
+    return true;
+}
+
+// Runs `body`, which returns false for a call that is not plain, with the status code in its argument.
+template <typename BODY>
+PyObject *guarded(BODY body)
+{
+    int rc = 0;
+    try {
+        if (!body(rc))
+            Py_RETURN_NONE;
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(rc);
+}
+
+// The library's call, with the interpreter free for other threads.
+template <typename CALL>
+int released(CALL call)
+{
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = call();
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
+void *current_stream()
+{
+    return c10::hip::getCurrentHIPStream().stream();
+}
+
+// (address, logits, ids, weights, renormalize)
+PyObject *route(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&](int &rc) {
+        int renormalize, type;
+        if (n != 5 || !truth(args[4], renormalize))
+            return false;
+        const auto fn = address<decltype(&gptq_w4a16_moe_route)>(args[0]);
+        const at::Tensor *logits = logits_of(args[1], type), *ids = plain(args[2], at::kInt, 2);
+        const at::Tensor *weights = plain(args[3], at::kFloat, 2);
+        if (!fn || !logits || !ids)
+            return false;
+        const int64_t M = logits->size(0), experts = logits->size(1), top_k = ids->size(1);
+        if (!fit({M, experts, top_k}) || !sizes(ids, {M, top_k}) || !sizes(weights, {M, top_k}))
+            return false;
+        void *const stream = current_stream();
+        rc = released([&] {
+            return fn(logits->data_ptr(), type, ids->data_ptr(), weights->data_ptr(), (int)M, (int)experts, (int)top_k, renormalize,
+                      stream);
+        });
+        return true;
+    });
+}
+
+// (address, x, logits, gate_up, down, out, top_k, group_size, renormalize)
+PyObject *moe(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&](int &rc) {
+        int top_k, group, renormalize, type;
+        if (n != 9 || !integer(args[6], top_k) || !integer(args[7], group) || !truth(args[8], renormalize))
+            return false;
+        const auto fn = address<decltype(&gptq_w4a16_moe)>(args[0]);
+        const at::Tensor *x = plain(args[1], at::kHalf, 2), *logits = logits_of(args[2], type);
+        const at::Tensor *out = plain(args[5], at::kHalf, 2);
+        gptq_w4a16_experts_t e;
+        if (!fn || !layer(x, args[3], args[4], out, group, e) || !sizes(logits, {x->size(0), e.experts}))
+            return false;
+        void *const stream = current_stream();
+        rc = released([&] {
+            return fn(x->data_ptr(), logits->data_ptr(), type, &e, out->data_ptr(), (int)x->size(0), top_k, renormalize,
+                      stream);
+        });
+        return true;
+    });
+}
+
+// (address, x, ids, weights, gate_up, down, out, group_size)
+PyObject *moe_experts(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&](int &rc) {
+        int group;
+        if (n != 8 || !integer(args[7], group))
+            return false;
+        const auto fn = address<decltype(&gptq_w4a16_moe_experts)>(args[0]);
+        const at::Tensor *x = plain(args[1], at::kHalf, 2), *ids = plain(args[2], at::kInt, 2);
+        const at::Tensor *weights = plain(args[3], at::kFloat, 2), *out = plain(args[6], at::kHalf, 2);
+        gptq_w4a16_experts_t e;
+        if (!fn || !ids || !layer(x, args[4], args[5], out, group, e))
+            return false;
+        const int64_t M = x->size(0), top_k = ids->size(1);
+        if (!fit({top_k}) || !sizes(ids, {M, top_k}) || !sizes(weights, {M, top_k}))
+            return false;
+        void *const stream = current_stream();
+        rc = released([&] {
+            return fn(x->data_ptr(), ids->data_ptr(), weights->data_ptr(), &e, out->data_ptr(), (int)M, (int)top_k, stream);
+        });
+        return true;
+    });
+}
+
+// (address, x, a, b, scaling, adapter, base, out)
+PyObject *lora_add(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&](int &rc) {
+        if (n != 8)
+            return false;
+        const auto fn = address<decltype(&gptq_w4a16_lora_add)>(args[0]);
+        int64_t ldx, ld_base, ld_out;
+        const at::Tensor *x = strided(args[1], ldx), *base = strided(args[6], ld_base), *out = strided(args[7], ld_out);
+        Adapters l;
+        if (!fn || !adapters(x, args + 2, out, l) || !sizes(base, {l.M, l.N}))
+            return false;
+        void *const stream = current_stream();
+        rc = released([&] {
+            return fn(x->data_ptr(), l.a, l.b, l.scaling, l.adapter, base->data_ptr(), out->data_ptr(), l.M, l.K, l.N, l.rank, l.count,
+                      (int)ldx, (int)ld_base, (int)ld_out, stream);
+        });
+        return true;
+    });
+}
+
+// (address, x, qweight, qzeros, scales, a, b, scaling, adapter, out, group_size)
+PyObject *gemm_lora(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&](int &rc) {
+        int group;
+        if (n != 11 || !integer(args[10], group) || group <= 0)
+            return false;
+        const auto fn = address<decltype(&gptq_w4a16_gemm_lora)>(args[0]);
+        const at::Tensor *x = plain(args[1], at::kHalf, 2), *qweight = plain(args[2], at::kInt, 2);
+        const at::Tensor *qzeros = plain(args[3], at::kInt, 2), *scales = plain(args[4], at::kHalf, 2);
+        const at::Tensor *out = plain(args[9], at::kHalf, 2);
+        Adapters l;
+        if (!fn || !adapters(x, args + 5, out, l) || l.K % group || l.K % 8 || l.N % 8 || !sizes(qweight, {l.K / 8, l.N}) ||
+            !sizes(qzeros, {l.K / group, l.N / 8}) || !sizes(scales, {l.K / group, l.N}))
+            return false;
+        void *const stream = current_stream();
+        rc = released([&] {
+            return fn(x->data_ptr(), qweight->data_ptr(), qzeros->data_ptr(), scales->data_ptr(), l.a, l.b, l.scaling, l.adapter,
+                      out->data_ptr(), l.M, l.K, l.N, group, l.rank, l.count, stream);
+        });
+        return true;
+    });
+}
+
+#define GPTQ_METHOD(name, doc)                                                                                                 \
+    {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL,                              \
+     #name doc " -> status code, or None for a call that is not plain"}
+
 PyMethodDef methods[] = {
     {"gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(gemm)), METH_FASTCALL,
      "gemm(address, x, qweight, qzeros, scales, index, out, group_size) -> status code, or None for a call that is not plain"},
+    GPTQ_METHOD(route, "(address, logits, ids, weights, renormalize)"),
+    GPTQ_METHOD(moe, "(address, x, logits, gate_up, down, out, top_k, group_size, renormalize)"),
+    GPTQ_METHOD(moe_experts, "(address, x, ids, weights, gate_up, down, out, group_size)"),
+    GPTQ_METHOD(lora_add, "(address, x, a, b, scaling, adapter, base, out)"),
+    GPTQ_METHOD(gemm_lora, "(address, x, qweight, qzeros, scales, a, b, scaling, adapter, out, group_size)"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -11,6 +11,7 @@ import ctypes
 
 import torch
 
+from . import binding
 from .binding import GptqError, _ptr, _stream, load
 
 EXPORTS = ("gptq_w4a16_moe_route", "gptq_w4a16_moe_experts", "gptq_w4a16_moe", "gptq_w4a16_moe_workspace_bytes",
@@ -28,9 +29,11 @@ class Experts(ctypes.Structure):
 
 
 _lib = None
+_addresses = {}  # of the entry points that the extension module calls
 
 
 def _load():
+    """The library with the argument types of this module's functions."""
     global _lib
     if _lib is None:
         lib = load()
@@ -46,8 +49,20 @@ def _load():
                 ("gptq_w4a16_lora_workspace_bytes", size, [ci] * 5)]:
             getattr(lib, name).restype = restype
             getattr(lib, name).argtypes = argtypes
+            _addresses[name] = ctypes.cast(getattr(lib, name), vp).value
         _lib = lib
     return _lib
+
+
+def _native(function, name, *args):
+    """Whether the extension module (csrc/native_call.cpp) has made the call; it leaves to the code below what is not plain."""
+    if _lib is None:
+        _load()
+    module = binding._native_module
+    rc = None if module is None else getattr(module, function)(_addresses[name], *args)
+    if rc:
+        raise GptqError(rc, name)
+    return rc == 0
 
 
 def _shape(t, shape, name):
@@ -87,6 +102,8 @@ def _experts(x, gate_up, down, out, group_size):
 
 def gptq_w4a16_moe_route(logits, ids, weights, renormalize: bool = True):
     """The top_k experts of every token and their softmax weights: fills ids [M, top_k] (int32) and weights (float32)."""
+    if _native("route", "gptq_w4a16_moe_route", logits, ids, weights, renormalize):
+        return ids, weights
     if logits.dim() != 2 or ids.dim() != 2:
         raise ValueError("logits must be [M, experts] and ids [M, top_k]")
     M, experts = logits.shape
@@ -103,6 +120,8 @@ def gptq_w4a16_moe_route(logits, ids, weights, renormalize: bool = True):
 
 def gptq_w4a16_moe_experts(x, ids, weights, gate_up, down, out, group_size: int):
     """out[M, hidden] = the weighted sum of every token's experts; an id outside [0, experts) adds nothing."""
+    if _native("moe_experts", "gptq_w4a16_moe_experts", x, ids, weights, gate_up, down, out, group_size):
+        return out
     layer, M = _experts(x, gate_up, down, out, group_size)
     if ids.dim() != 2:
         raise ValueError("ids must be [M, top_k]")
@@ -119,6 +138,8 @@ def gptq_w4a16_moe_experts(x, ids, weights, gate_up, down, out, group_size: int)
 
 def gptq_w4a16_moe(x, logits, gate_up, down, out, top_k: int, group_size: int, renormalize: bool = True):
     """The whole layer: routing by `logits` [M, experts], then the experts."""
+    if _native("moe", "gptq_w4a16_moe", x, logits, gate_up, down, out, top_k, group_size, renormalize):
+        return out
     layer, M = _experts(x, gate_up, down, out, group_size)
     _shape(logits, (M, layer.experts), "logits")
     pointer, kind = _logits(logits)
@@ -168,6 +189,8 @@ def _adapters(x, a, b, scaling, adapter, out):
 def gptq_w4a16_lora_add(x, a, b, scaling, adapter, base, out):
     """out[m] = base[m] + scaling[l] * (x[m] @ a[l].T) @ b[l].T with l = adapter[m], or base[m] where l is no adapter.
     The rows of x, base and out may be strided; out may be base."""
+    if _native("lora_add", "gptq_w4a16_lora_add", x, a, b, scaling, adapter, base, out):
+        return out
     pointers, M, K, N, rank, adapters = _adapters(x, a, b, scaling, adapter, out)
     _shape(base, (M, N), "base")
     px, ldx = _rows(x, "x")
@@ -181,6 +204,8 @@ def gptq_w4a16_lora_add(x, a, b, scaling, adapter, base, out):
 
 def gptq_w4a16_gemm_lora(x, qweight, qzeros, scales, a, b, scaling, adapter, out, group_size: int):
     """out = x @ W (gptq_w4a16_gemm) with every row's adapter on top."""
+    if _native("gemm_lora", "gptq_w4a16_gemm_lora", x, qweight, qzeros, scales, a, b, scaling, adapter, out, group_size):
+        return out
     pointers, M, K, N, rank, adapters = _adapters(x, a, b, scaling, adapter, out)
     group_size = int(group_size)
     if group_size <= 0 or K % group_size or K % 8 or N % 8:

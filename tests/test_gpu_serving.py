@@ -322,3 +322,53 @@ def test_gemm_lora_is_the_product_with_the_adapters_on_top(S, M, K, N, group, ra
     binding.gptq_w4a16_gemm(cuda(x), *packed, None, base, group)
     want, off = lora64(x, a, b, scaling, adapter, base.cpu().numpy())
     inside(out.cpu().numpy(), want, off, "gemm_lora")
+
+
+# ---- marshalling ----
+
+def test_calls_through_the_extension_module_and_without_it_agree(S, monkeypatch):
+    """Plain calls go through the module; what it leaves aside, and everything where it is absent, through Python."""
+    from paper_2511_19438_amd import binding
+
+    if binding._native_module is None:
+        pytest.skip("the extension module was not built for this torch")
+    rng = np.random.default_rng(11)
+    M, hidden, inter, E, top_k, group, rank = 3, 128, 64, 4, 2, 32, 8
+    gate_up, down = (tuple(map(cuda, t)) for t in layer(rng, hidden, inter, E, group))
+    x = cuda(rng.standard_normal((M, hidden)).astype(np.float16))
+    logits = cuda(rng.standard_normal((M, E)).astype(np.float32))
+    packed = tuple(map(cuda, random_packed(rng, hidden, inter, group)))
+    a, b, scaling = map(cuda, adapters(rng, 3, rank, hidden, inter))
+    adapter = torch.tensor([2, -1, 0], dtype=torch.int32, device="cuda")
+
+    def results(calls):
+        ids, weights = torch.empty(M, top_k, dtype=torch.int32, device="cuda"), torch.empty(M, top_k, device="cuda")
+        S.gptq_w4a16_moe_route(logits, ids, weights, False)
+        outs = [torch.empty(M, hidden, dtype=torch.float16, device="cuda") for _ in range(2)]
+        S.gptq_w4a16_moe(x, logits, gate_up, down, outs[0], top_k, group)
+        S.gptq_w4a16_moe_experts(x, ids, weights, gate_up, down, outs[1], group)
+        sums = [torch.empty(M, inter, dtype=torch.float16, device="cuda") for _ in range(2)]
+        S.gptq_w4a16_gemm_lora(x, *packed, a, b, scaling, adapter, sums[0], group)
+        S.gptq_w4a16_lora_add(x, a, b, scaling, adapter, sums[0], sums[1])
+        return [ids, weights, *outs, *sums]
+
+    taken = []
+    inner = S._native
+    monkeypatch.setattr(S, "_native", lambda *args: taken.append(inner(*args)) or taken[-1])
+    with_module = results(taken)
+    assert taken == [True] * 5
+    monkeypatch.setattr(binding, "_native_module", None)
+    without = results(taken)
+    assert taken[5:] == [False] * 5
+    for one, other in zip(with_module, without):
+        assert torch.equal(one, other)
+    monkeypatch.undo()
+    # what is not plain: a list for a tuple, a number for a truth value; refusals of the library keep their code
+    out = torch.empty(M, hidden, dtype=torch.float16, device="cuda")
+    S.gptq_w4a16_moe(x, logits, list(gate_up), down, out, top_k, group, 1)
+    assert torch.equal(out, with_module[2])
+    with pytest.raises(binding.GptqError) as e:
+        S.gptq_w4a16_moe(x, logits, gate_up, down, out, E + 1, group)
+    assert e.value.code == -2
+    with pytest.raises(ValueError, match="out must be"):
+        S.gptq_w4a16_moe(x, logits, gate_up, down, out[:, :64], top_k, group)
