@@ -13,15 +13,17 @@ namespace {
 //   20 of 2048x2048, 16 tokens: 128 columns 17, 64 13
 //   8 of 11008x4096, 64 tokens: 64 columns of four wavefronts 47, 32 of eight 62; 2 of them, one token: 23 and 13
 template <bool DOWN>
-hipError_t product(Args &a, Shape s, double hit, hipStream_t stream)
+hipError_t product(Args &a, Shape s, double hit, int group_size, hipStream_t stream)
 {
     const int wide = DOWN ? 64 : 128;
-    s.wide = hit * ((a.N + wide - 1) / wide) >= (DOWN ? 256 : 512);
+    s.wide = hit * ((a.N + wide - 1) / wide) >= (DOWN ? 256 : 1024);
     const int cols = s.wide ? wide : wide / 2;
     a.tiles = (a.N + cols - 1) / cols;
-    if (a.group_size % 128 == 0)
+    a.groups = a.K / group_size;
+    a.per_group = group_size / 32;
+    if (group_size % 128 == 0)
         return launch_product<0, DOWN>(a, s, stream);
-    if (a.group_size % 64 == 0)
+    if (group_size % 64 == 0)
         return launch_product<1, DOWN>(a, s, stream);
     return launch_product<2, DOWN>(a, s, stream);
 }
@@ -73,10 +75,10 @@ hipError_t launch_experts(const Call &c, const Layout &l, unsigned char *scratch
         s.groups = c.top_k;
     } else if (pairs <= kDirectPairs && c.experts <= kDirectExperts) {
         a.mode = kDirect;
-        // workgroups for twice the tokens that an expert has on average; they take what is more in turns
+        // workgroups for one and a half times the tokens that an expert has on average; they take what is more in turns
         const int most = (c.M + s.rows - 1) / s.rows;
-        a.chunks = 1 + 2 * pairs / c.experts / s.rows;
-        a.chunks = a.chunks < most ? a.chunks : most;
+        a.chunks = (3 * pairs / (2 * c.experts) + s.rows - 1) / s.rows;
+        a.chunks = a.chunks < 1 ? 1 : a.chunks < most ? a.chunks : most;
         s.groups = c.experts * a.chunks;
     } else {
         a.mode = kGrouped;
@@ -107,12 +109,12 @@ hipError_t launch_experts(const Call &c, const Layout &l, unsigned char *scratch
     a.top_k = c.top_k;
     a.K = c.hidden;
     a.N = 2 * c.inter;
-    a.group_size = c.group_size;
     a.experts = c.experts;
+    a.token_of = (1u << kTokenShift) / c.top_k + 1;
     // experts that tokens who choose alike would hit
     const double share = c.top_k < c.experts ? (double)c.top_k / c.experts : 1.0;
     const double hit = c.experts * (1.0 - std::pow(1.0 - share, c.M));
-    err = product<false>(a, s, hit, stream);
+    err = product<false>(a, s, hit, c.group_size, stream);
     if (err != hipSuccess)
         return err;
     a.x = a.hidden;
@@ -121,7 +123,7 @@ hipError_t launch_experts(const Call &c, const Layout &l, unsigned char *scratch
     a.scales = c.down_scales;
     a.K = c.inter;
     a.N = c.hidden;
-    return product<true>(a, s, hit, stream);
+    return product<true>(a, s, hit, c.group_size, stream);
 }
 
 }  // namespace moe

@@ -53,8 +53,13 @@ struct Args {
     float *partial;          // down: [pairs, N]
     half_t *out;             // down: [M, N]
     unsigned *counters;      // down: one per column tile, zero between launches
-    int M, top_k, K, N, group_size, experts, tiles, mode, chunks, logits_fp32, renormalize;
+    int M, top_k, K, N, experts, tiles, mode, chunks, logits_fp32, renormalize;
+    int groups;            // of a matrix: K / group_size
+    int per_group;         // group_size / 32
+    uint32_t token_of;     // pair / top_k = pair * token_of >> kTokenShift
 };
+
+constexpr int kTokenShift = 19;  // exact for pairs below 4096 and up to 32 of a token: 4096 * 32 <= 2^19
 
 // What a launch is made of.
 struct Shape {
@@ -144,17 +149,16 @@ __device__ __forceinline__ void stream_weights(const Args &a, int expert, int ti
         const int row = 8 * q + (lane >> 3);
         const int pair = pairs[min(row, count - 1)];
         const uint32_t chunk = (lane & 7) ^ (row >> 1 & 7);
-        const uint32_t base = (uint32_t)(DOWN ? pair : pair / a.top_k) * K;
+        const uint32_t base = (DOWN ? (uint32_t)pair : (uint32_t)pair * a.token_of >> kTokenShift) * K;
         off_x[q] = (base + chunk * 8) * 2u;
         off_x_last[q] = (base + (chunk & 3) * 8) * 2u;
     }
-    const size_t groups = K / a.group_size;
     const uint32_t *const qweight = a.qweight + (size_t)expert * (K / 8) * N;
     const char *w_next = reinterpret_cast<const char *>(qweight + (size_t)b0 * UNIT * 8 * N);
     const char *x_next = reinterpret_cast<const char *>(a.x + (size_t)b0 * UNIT * 64);
     const size_t w_step = (size_t)N * 32;
     // scales and zero points: the row of scales of the next step that needs one, and its place in its group, in 32 k
-    const int per_group = a.group_size / 32;
+    const int per_group = a.per_group;
     constexpr int kSpan = SC == kPairs ? 4 : SC == kStages ? 2 : 1;  // steps that one load of a row serves
     int group = b0 * UNIT * 2 / per_group;
     int in_group = b0 * UNIT * 2 - group * per_group;
@@ -165,7 +169,7 @@ __device__ __forceinline__ void stream_weights(const Args &a, int expert, int ti
         const int i = 64 * j + lane;
         const bool scales = i < COLS / 2;
         const int n = scales ? column<COLS, DOWN>(tile, 2 * i, 2, N) : column<COLS, DOWN>(tile, 8 * min(i - COLS / 2, COLS / 8 - 1), 8, N);
-        const size_t at = ((size_t)expert * groups + group) * N + n;
+        const size_t at = ((size_t)expert * a.groups + group) * N + n;
         sz_next[j] = scales ? reinterpret_cast<const char *>(a.scales + at) : reinterpret_cast<const char *>(a.qzeros + at / 8);
         sz_step[j] = scales ? (uint32_t)N * 2u : (uint32_t)N / 2u;
     }
@@ -355,6 +359,8 @@ __device__ __forceinline__ void stream_weights(const Args &a, int expert, int ti
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
+            if (16 * i + 4 * kg + r >= count)
+                continue;
             float *row = red + ((size_t)wave * ROWS + 16 * i + 4 * kg + r) * COLS;
 #pragma unroll
             for (int c = 0; c < NF; ++c)
@@ -414,12 +420,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
         step = a.chunks * MAXROWS;
 #pragma unroll
         for (int i = 0; i < kDirectPairs / 64; ++i)
-            id[i] = 64 * i + lane < all_pairs ? a.ids[64 * i + lane] : -1;
+            if (64 * i < all_pairs)  // (uniform)
+                id[i] = a.ids[min(64 * i + lane, all_pairs - 1)];
 #pragma unroll
-        for (int i = 0; i < kDirectPairs / 64; ++i) {
-            found += __popcll(__ballot(id[i] == expert));
-            total_pairs += __popcll(__ballot(id[i] >= 0 && id[i] < a.experts));
-        }
+        for (int i = 0; i < kDirectPairs / 64; ++i)
+            if (64 * i < all_pairs) {
+                if (64 * i + lane >= all_pairs)
+                    id[i] = -1;
+                found += __popcll(__ballot(id[i] == expert));
+                if (DOWN)
+                    total_pairs += __popcll(__ballot((uint32_t)id[i] < (uint32_t)a.experts));
+            }
     } else {
         total_pairs = a.grouping->pairs;
         if (u < a.grouping->units) {
@@ -442,6 +453,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
             int before = 0;
 #pragma unroll
             for (int i = 0; i < kDirectPairs / 64; ++i) {
+                if (64 * i >= all_pairs)
+                    break;
                 const uint64_t match = __ballot(id[i] == expert);
                 const int place = before + __popcll(match & ((1ull << lane) - 1)) - first;
                 if (id[i] == expert && place >= 0 && place < count)
