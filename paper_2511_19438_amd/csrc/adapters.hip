@@ -256,7 +256,7 @@ struct Operand {
 //      rows in fours, 16 columns that stand together: full lines on both sides.  (The other way round, a lane with four rows
 //      of four columns: 512 rows of 12288 columns at rank 32 14.2 us, here 12.3.) ----
 template <int CHUNKS>
-__global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(const Args a)
+__global__ __launch_bounds__(kThreads, CHUNKS == 1 ? 4 : CHUNKS == 2 ? 3 : CHUNKS == 4 ? 2 : 1) void expand_kernel(const Args a)
 {
     constexpr int PER = 2 * CHUNKS;  // ranks of a row that a thread brings to LDS
     constexpr int TILES = 4;
@@ -271,10 +271,12 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
         return;
     const int owner = __shfl(mine, cq);
 
-    half8_t bv[TILES][CHUNKS];
+    // B of an adapter; of up to 128 ranks that of the next one, too, which is on its way while this one is multiplied
+    constexpr int AHEAD = CHUNKS <= 4 ? 1 : 0;
+    half8_t bv[1 + AHEAD][TILES][CHUNKS];
     half8_t base[2];
     int n0;
-    auto load_adapter = [&](int l) {
+    auto load_adapter = [&](int l, half8_t (&bv)[TILES][CHUNKS]) {
         const half_t *lb = a.b + (size_t)l * a.N * a.rank;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
         n0 = (tile * kWaves + wave) * 16 * TILES;
         const int l = left ? next_adapter(mine, left) : -1;
         if (l >= 0)
-            load_adapter(l);
+            load_adapter(l, bv[0]);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             base[h] = *reinterpret_cast<const half8_t *>(base_row + min(n0 + 16 * kg + 8 * h, a.N - 8));
@@ -325,7 +327,7 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
             acc[t] = float4_t{0.f, 0.f, 0.f, 0.f};
-        while (l >= 0) {
+        auto multiply = [&](const half8_t (&bv)[TILES][CHUNKS]) {
             const bool chosen = owner == l;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
@@ -339,10 +341,19 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
                 for (int r = 0; r < 4; ++r)
                     acc[t][r] = chosen ? d[r] : acc[t][r];
             }
-            l = -1;
-            if (left) {
-                l = next_adapter(mine, left);
-                load_adapter(l);
+        };
+        while (l >= 0) {
+#pragma unroll
+            for (int i = 0; i <= AHEAD; ++i) {
+                if (l < 0)
+                    break;
+                const int next = left ? next_adapter(mine, left) : -1;
+                if (AHEAD && next >= 0)
+                    load_adapter(next, bv[(i + 1) % (1 + AHEAD)]);
+                multiply(bv[i]);
+                if (!AHEAD && next >= 0)
+                    load_adapter(next, bv[0]);
+                l = next;
             }
         }
 #pragma unroll
@@ -365,17 +376,25 @@ __global__ __launch_bounds__(kThreads, CHUNKS > 4 ? 2 : 4) void expand_kernel(co
     }
 }
 
-constexpr int kFewRows = 64;
-
 int row_tiles(int M)
 {
     return (M + kRows - 1) / kRows;
 }
 
-// Workgroups along the adapters of a tile.  A decode step's rows mostly have their own each, a prompt's few.
+// Workgroups along the adapters of a tile.  A decode step's rows mostly have their own each, a prompt's few; those without an
+// adapter are a little time, an adapter more to a workgroup is another wait.
 int adapter_slots(int M)
 {
-    return M < kRows ? M : M <= kFewRows ? kRows : 4;
+    return M < kRows ? M : M <= 64 ? kRows : M <= 256 ? 8 : 4;
+}
+
+// Whether the second product takes a row to a workgroup.  It then reads B once for every row, from L2 mostly, where tiles read
+// it once for rows that share an adapter and wait for one adapter after the other where they do not.  us, by rows and by
+// tiles: decode steps, 32 rows of 12288 columns at rank 16 3.5, 9.8; 64 of 8192 at 64 13.2, 21.8; 77 of 6888 at 24, five
+// adapters 4.8, 6.3.  Prompts: 128 rows of 12288 at 16 8.0, 5.1 (rows of 64 adapters 9.0, 14.0); 512 of 12288 at 32 33.5, 12.3.
+bool row_by_row(int M, int N, int rank)
+{
+    return M <= 64 || (long long)M * N * rank <= 1ll << 24;
 }
 
 // Slices of K: 512 k each, which a workgroup loads at once, while the workgroups are no more than twice the compute units.
@@ -451,14 +470,16 @@ hipError_t launch_lora(const Call &c, void *scratch, hipStream_t stream)
     const int steps = (c.K + 31) / 32;
     a.slices = k_slices(c.M, c.K);
     a.slice_steps = (steps + a.slices - 1) / a.slices;
-    if (c.M <= kFewRows) {
+    if (c.M <= 64 || c.rank <= 16)
         launch_shrink<1, 4>(a, stream);
+    else
+        launch_shrink<2, 4>(a, stream);
+    if (row_by_row(c.M, c.N, c.rank)) {
         launch_expand_rows<1>(a, stream);
     } else {
         // one turn of 256 columns to a workgroup until there are eight workgroups to a compute unit
         const int tiles = (c.N + 255) / 256, turns = (int)(((long long)tiles * a.row_tiles + 2047) / 2048);
         a.col_groups = (tiles + turns - 1) / turns;
-        launch_shrink<2, 4>(a, stream);
         launch_expand(a, stream);
     }
     return hipGetLastError();
