@@ -7,17 +7,25 @@ namespace gptq {
 namespace moe {
 namespace {
 
-// Columns of a workgroup: the wide ones read longer runs of memory and need fewer activations per weight, but want
-// workgroups enough.  us of gate and up and of down, at the experts that a call is expected to hit:
-//   8 of 4096x22016, 64 tokens: 128 columns 80, 64 98; 2 of them, one token: 21 and 21
-//   20 of 2048x2048, 16 tokens: 128 columns 17, 64 13
-//   8 of 11008x4096, 64 tokens: 64 columns of four wavefronts 47, 32 of eight 62; 2 of them, one token: 23 and 13
+// Columns of a workgroup: the wide ones read longer runs of memory and need fewer activations per weight, but want workgroups
+// enough; where there are few, more wavefronts have more of them under way at once.  us, at the experts that a call is expected
+// to hit ("workgroups": of 64 columns):
+//   gate and up   8 of 4096x22016, 64 tokens (2752 workgroups): 128 columns 80, 64 98; 2 of them, one token (688) 21, 21;
+//                 20 of 2048x2048, 16 tokens (1300) 17, 13
+//                 the layer, with four wavefronts and with eight: 2 of 8192x4096 (224) 27.6, 26.4; 4 of 2048x2048 (128) 14.1,
+//                 13.5; 8 of 4768x2176, groups of 32 (272) 46.1, 50.4
+//                 the layer, with 64 columns and with 32: 2 of 4096x2048 (64) 14.0, 13.2; 1 of 8192x2048 (32) 17.2, 15.0; 2 of
+//                 8192x4096 (224) 30, 36
+//   down          8 of 11008x4096, 64 tokens (512): 64 columns and four wavefronts 47, 32 and eight 62; 2 of them (128) 23, 13
 template <bool DOWN>
 hipError_t product(Args &a, Shape s, double hit, int group_size, hipStream_t stream)
 {
-    const int wide = DOWN ? 64 : 128;
-    s.wide = hit * ((a.N + wide - 1) / wide) >= (DOWN ? 256 : 1024);
-    const int cols = s.wide ? wide : wide / 2;
+    const double workgroups = hit * ((a.N + 63) / 64);  // of 64 columns
+    if (DOWN)
+        s.width = workgroups >= 256 ? kMiddle : kNarrowest;
+    else
+        s.width = workgroups >= 2048 ? kWide : workgroups >= 256 ? kMiddle : workgroups >= 128 ? kNarrow : kNarrowest;
+    const int cols = s.width == kWide ? 128 : s.width == kNarrowest ? 32 : 64;
     a.tiles = (a.N + cols - 1) / cols;
     a.groups = a.K / group_size;
     a.per_group = group_size / 32;

@@ -61,10 +61,14 @@ struct Args {
 
 constexpr int kTokenShift = 19;  // exact for pairs below 4096 and up to 32 of a token: 4096 * 32 <= 2^19
 
+// Columns of a workgroup, its wavefronts and the stages of a ring.  Gate and up: 128, 4, 2; 64, 4, 2; 64, 8, 2; 32, 8, 3.
+// Down: 64, 4, 3 (middle) and 32, 8, 3 (narrowest).
+enum Width { kWide, kMiddle, kNarrow, kNarrowest };
+
 // What a launch is made of.
 struct Shape {
     int rows;    // of a workgroup at a time: 8, 16 or 32
-    bool wide;   // 128 columns (gate and up) or 64 (down) of a workgroup, four wavefronts; else 64, or 32 and eight wavefronts
+    int width;   // see above
     int groups;  // of workgroups, one for each tile
 };
 
@@ -108,7 +112,7 @@ __device__ __forceinline__ int column(int tile, int c, int width, int N)
 
 // The sums of `count` pairs with the tile's columns, over each wavefront's share of K: red [WAVES][ROWS][COLS].
 // TM: 16-row blocks; LX: DMA instructions of the activations (8 rows each).  Rows past the last pair repeat it.
-template <int TM, int LX, int COLS, int WAVES, Scaling SC, int DEPTH, bool DOWN>
+template <int TM, int LX, int COLS, int WAVES, Scaling SC, int DEPTH, bool DOWN, bool FRESH>
 __device__ __forceinline__ void stream_weights(const Args &a, int expert, int tile, const int32_t *pairs, int count,
                                                unsigned char *smem)
 {
@@ -124,7 +128,12 @@ __device__ __forceinline__ void stream_weights(const Args &a, int expert, int ti
     constexpr int QUADS = COLS / 4;
     static_assert(DEPTH == 2 || DEPTH == 3, "the waits below");
     static_assert(COLS == 32 || COLS == 64 || COLS == 128, "whole DMA instructions, whole zero words on both sides");
-    const int lane = threadIdx.x & 63;
+    // Addresses are computed before an expert's tokens are known, for all numbers of rows at once, while the ids come in (16
+    // tokens over 64 experts 25.7 us, otherwise 27.7).  Where registers are short that would spill them: the number of the lane
+    // comes from nowhere then (64 tokens of 8 experts 141 us, so 138).
+    int lane = threadIdx.x & 63;
+    if (FRESH)
+        asm volatile("" : "+v"(lane));
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int cq = lane & 15;
     const int kg = lane >> 4;
@@ -162,16 +171,22 @@ __device__ __forceinline__ void stream_weights(const Args &a, int expert, int ti
     constexpr int kSpan = SC == kPairs ? 4 : SC == kStages ? 2 : 1;  // steps that one load of a row serves
     int group = b0 * UNIT * 2 / per_group;
     int in_group = b0 * UNIT * 2 - group * per_group;
-    const char *sz_next[S::SZ_LOADS];
-    uint32_t sz_step[S::SZ_LOADS];
-#pragma unroll
-    for (int j = 0; j < S::SZ_LOADS; ++j) {
-        const int i = 64 * j + lane;
-        const bool scales = i < COLS / 2;
-        const int n = scales ? column<COLS, DOWN>(tile, 2 * i, 2, N) : column<COLS, DOWN>(tile, 8 * min(i - COLS / 2, COLS / 8 - 1), 8, N);
-        const size_t at = ((size_t)expert * a.groups + group) * N + n;
-        sz_next[j] = scales ? reinterpret_cast<const char *>(a.scales + at) : reinterpret_cast<const char *>(a.qzeros + at / 8);
-        sz_step[j] = scales ? (uint32_t)N * 2u : (uint32_t)N / 2u;
+    // 128 columns take an instruction for the scales and one for the zero points, each from a uniform base; fewer take one
+    // for both, from an address per lane.
+    const size_t sz_at = ((size_t)expert * a.groups + group) * N;
+    const char *sc_next = reinterpret_cast<const char *>(a.scales + sz_at);
+    const char *zp_next = reinterpret_cast<const char *>(a.qzeros + sz_at / 8);
+    uint32_t off_s, off_z, lane_step;
+    const char *lane_next;
+    if constexpr (COLS == 128) {
+        off_s = column<COLS, DOWN>(tile, 2 * lane, 2, N) * 2u;
+        off_z = column<COLS, DOWN>(tile, 8 * min(lane, COLS / 8 - 1), 8, N) / 2u;
+    } else {
+        const bool scale = lane < COLS / 2;
+        const int n = scale ? column<COLS, DOWN>(tile, 2 * lane, 2, N)
+                            : column<COLS, DOWN>(tile, 8 * min(lane - COLS / 2, COLS / 8 - 1), 8, N);
+        lane_next = scale ? sc_next + n * 2u : zp_next + n / 2u;
+        lane_step = scale ? (uint32_t)N * 2u : (uint32_t)N / 2u;
     }
 
     const unsigned char *const ring = smem + (size_t)wave * (DEPTH * S::BYTES);
@@ -193,10 +208,15 @@ __device__ __forceinline__ void stream_weights(const Args &a, int expert, int ti
                 in_group = step ? 0 : in_group;
                 if (half && g == 0)  // nothing behind it: the second row is the first again
                     step = false;
-#pragma unroll
-                for (int j = 0; j < S::SZ_LOADS; ++j) {
-                    dma_4(put + S::W_BYTES + S::X_BYTES + g * S::SZ_BYTES + j * 256, sz_next[j]);
-                    sz_next[j] += step ? sz_step[j] : 0u;
+const uint32_t at = put + S::W_BYTES + S::X_BYTES + g * S::SZ_BYTES;
+                if constexpr (COLS == 128) {
+                    dma_4(at, off_s, sc_next);
+                    dma_4(at + 256, off_z, zp_next);
+                    sc_next += step ? (size_t)N * 2 : 0;
+                    zp_next += step ? (size_t)N / 2 : 0;
+                } else {
+                    dma_4(at, lane_next);
+                    lane_next += step ? lane_step : 0u;
                 }
             }
         }
@@ -252,6 +272,7 @@ __device__ __forceinline__ void stream_weights(const Args &a, int expert, int ti
         for (int b = b0; b < b1; ++b) {
             float4_t d[TM][NT];
             half2_t neg_lo[NT], neg_hi[NT];
+            half2_t pairs_of_scales[NT / 2];
             float sf[NT];
 #pragma unroll
             for (int s = 0; s < UNIT; ++s) {
@@ -290,17 +311,18 @@ __device__ __forceinline__ void stream_weights(const Args &a, int expert, int ti
                             const int col = c < NF ? c * 64 + 4 * cq : NF * 64 + 2 * cq;
                             const uint32_t zeros =
                                 *reinterpret_cast<const uint32_t *>(sz + COLS * 2 + (col >> 3) * 4) >> (4 * (col & 7));
-                            uint32_t pair[2];
-                            pair[0] = *reinterpret_cast<const uint32_t *>(sz + col * 2);
-                            pair[1] = c < NF ? *reinterpret_cast<const uint32_t *>(sz + col * 2 + 4) : 0u;
+                            pairs_of_scales[2 * c] = as_half2(*reinterpret_cast<const uint32_t *>(sz + col * 2));
+                            if (c < NF)
+                                pairs_of_scales[2 * c + 1] = as_half2(*reinterpret_cast<const uint32_t *>(sz + col * 2 + 4));
 #pragma unroll
                             for (int j = 0; j < (c < NF ? 4 : 2); ++j) {
                                 const uint32_t z = zeros >> (4 * j) & 15u;
                                 const uint32_t zz = z | (z << 16);
                                 neg_lo[4 * c + j] = as_half2(zz | 0xE400E400u);         // (-(1024 + z)) x2
                                 neg_hi[4 * c + j] = as_half2((zz << 4) | 0xD400D400u);  // (-(64 + z)) x2
-                                const uint16_t bits = (uint16_t)((j & 1) ? pair[j / 2] >> 16 : pair[j / 2] & 0xffffu);
-                                sf[4 * c + j] = (float)__builtin_bit_cast(half_t, bits);
+                                sf[4 * c + j] = (float)pairs_of_scales[2 * c + j / 2][j % 2];
+                                if (!FRESH)  // (else the multiply-add takes fp16, at half the rate and for half the registers)
+                                    asm("" : "+v"(sf[4 * c + j]));
                             }
                         }
                     }
@@ -377,6 +399,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
 {
     constexpr int kThreads = 64 * WAVES;
     constexpr int QUADS = COLS / 4;
+    constexpr bool kFresh = COLS == 128 && MAXROWS == 32;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int32_t s_pairs[WAVES][MAXROWS];  // every wavefront finds the pairs for itself
     __shared__ int s_last;
@@ -391,6 +414,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
     int expert = 0, found = 0, total_pairs = 0;  // of the workgroup's group; of the call
     int first = 0, step = MAXROWS;               // found pairs that this workgroup begins with, and goes on by
     int32_t id[kDirectPairs / 64];               // kDirect: a lane's ids
+    auto load_ids = [&](int lane) {
+#pragma unroll
+        for (int i = 0; i < kDirectPairs / 64; ++i)
+            if (64 * i < all_pairs)  // (uniform)
+                id[i] = a.ids[min(64 * i + lane, all_pairs - 1)];
+#pragma unroll
+        for (int i = 0; i < kDirectPairs / 64; ++i)
+            if (64 * i < all_pairs && 64 * i + lane >= all_pairs)
+                id[i] = -1;
+    };
     if (a.mode == kOneToken) {
         int32_t mine;
         if (!DOWN && a.logits) {
@@ -418,15 +451,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
         expert = u / a.chunks;
         first = (u - expert * a.chunks) * MAXROWS;
         step = a.chunks * MAXROWS;
-#pragma unroll
-        for (int i = 0; i < kDirectPairs / 64; ++i)
-            if (64 * i < all_pairs)  // (uniform)
-                id[i] = a.ids[min(64 * i + lane, all_pairs - 1)];
+        load_ids(lane);
 #pragma unroll
         for (int i = 0; i < kDirectPairs / 64; ++i)
             if (64 * i < all_pairs) {
-                if (64 * i + lane >= all_pairs)
-                    id[i] = -1;
                 found += __popcll(__ballot(id[i] == expert));
                 if (DOWN)
                     total_pairs += __popcll(__ballot((uint32_t)id[i] < (uint32_t)a.experts));
@@ -450,6 +478,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
     for (; first < found; first += step) {
         const int count = min(found - first, MAXROWS);
         if (a.mode == kDirect) {
+            if (kFresh && done) {
+                int again = lane;
+                asm volatile("" : "+v"(again));
+                load_ids(again);
+            }
             int before = 0;
 #pragma unroll
             for (int i = 0; i < kDirectPairs / 64; ++i) {
@@ -465,14 +498,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
         if (done)
             __syncthreads();  // the sums of the pairs before have been read
         if (MAXROWS <= 8 || count <= 8)
-            stream_weights<1, 1, COLS, WAVES, SC, DEPTH, DOWN>(a, expert, tile, pairs, count, smem);
+            stream_weights<1, 1, COLS, WAVES, SC, DEPTH, DOWN, kFresh>(a, expert, tile, pairs, count, smem);
         else if (MAXROWS <= 16 || count <= 16)
-            stream_weights<1, MAXROWS <= 8 ? 1 : 2, COLS, WAVES, SC, DEPTH, DOWN>(a, expert, tile, pairs, count, smem);
+            stream_weights<1, MAXROWS <= 8 ? 1 : 2, COLS, WAVES, SC, DEPTH, DOWN, kFresh>(a, expert, tile, pairs, count, smem);
         else if (count <= 24)
-            stream_weights<MAXROWS <= 16 ? 1 : 2, MAXROWS <= 16 ? 1 : 3, COLS, WAVES, SC, DEPTH, DOWN>(a, expert, tile, pairs,
+            stream_weights<MAXROWS <= 16 ? 1 : 2, MAXROWS <= 16 ? 1 : 3, COLS, WAVES, SC, DEPTH, DOWN, kFresh>(a, expert, tile, pairs,
                                                                                                        count, smem);
         else
-            stream_weights<MAXROWS <= 16 ? 1 : 2, MAXROWS <= 16 ? 1 : 4, COLS, WAVES, SC, DEPTH, DOWN>(a, expert, tile, pairs,
+            stream_weights<MAXROWS <= 16 ? 1 : 2, MAXROWS <= 16 ? 1 : 4, COLS, WAVES, SC, DEPTH, DOWN, kFresh>(a, expert, tile, pairs,
                                                                                                        count, smem);
         const int rows = count <= 16 ? 16 : 32;
         __syncthreads();
@@ -516,7 +549,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void experts_kernel(const Args a)
     __builtin_amdgcn_s_waitcnt(0);  // every partial store of this workgroup has been acknowledged
     __syncthreads();
     if (tid == 0)
-        s_last = (int)slice_arrive(a.counters + tile, (unsigned)done) + done == total_pairs;
+        s_last = (int)slice_arrive(a.counters + tile, (unsigned)__builtin_amdgcn_readfirstlane(done)) + done == total_pairs;
     __syncthreads();
     if (!s_last)
         return;

@@ -46,9 +46,12 @@ template <>
 hipError_t launch_product<GPTQ_EXPERTS_SCALING, kDown>(const Args &a, const Shape &s, hipStream_t stream)
 {
     if constexpr (kDown)
-        return s.wide ? launch_rows<64, 4, 3>(a, s, stream) : launch_rows<32, 8, 3>(a, s, stream);
+        return s.width == kNarrowest ? launch_rows<32, 8, 3>(a, s, stream) : launch_rows<64, 4, 3>(a, s, stream);
     else
-        return s.wide ? launch_rows<128, 4, 2>(a, s, stream) : launch_rows<64, 4, 2>(a, s, stream);
+        return s.width == kWide     ? launch_rows<128, 4, 2>(a, s, stream)
+               : s.width == kMiddle ? launch_rows<64, 4, 2>(a, s, stream)
+               : s.width == kNarrow ? launch_rows<64, 8, 2>(a, s, stream)
+                                    : launch_rows<32, 8, 3>(a, s, stream);
 }
 
 }  // namespace moe

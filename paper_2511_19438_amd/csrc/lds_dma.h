@@ -41,6 +41,12 @@ __device__ __forceinline__ void dma_4(uint32_t lds, const char *src)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory");
 }
+// The same from base + byte_off, the base uniform over the wavefront.
+__device__ __forceinline__ void dma_4(uint32_t lds, uint32_t byte_off, const char *base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(byte_off), "s"(base)
+                 : "memory");
+}
 
 // All but the last N of this wavefront's loads have arrived.
 template <int N>
