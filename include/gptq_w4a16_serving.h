@@ -56,7 +56,7 @@ typedef struct gptq_w4a16_experts {
  * without any gets zeros.  Sums are fp32; the product of gate and up is rounded to fp16 (like any activation between two
  * products of this library: values beyond 65504 become infinite), the result once.  Only experts that a token is sent to
  * are read, once for every 32 of their tokens, so the call is meant for the tokens of decode steps: M * top_k <= 4096,
- * top_k <= 32, experts <= 1024, hidden and inter <= 2^20, M * hidden and M * top_k * inter < 2^31 (else
+ * top_k <= 32, experts <= 1024, hidden and inter <= 2^18, M * hidden and M * top_k * inter < 2^31 (else
  * GPTQ_UNSUPPORTED_SHAPE).
  * `out` may not overlap x.
  */
@@ -86,7 +86,7 @@ GPTQ_API size_t gptq_w4a16_moe_workspace_bytes(int M, int hidden, int inter, int
  *     out      fp16  [M, N], rows ld_out elements apart; may be base itself (then ld_out == ld_base), no other overlap
  * x A^T is summed and kept in fp32 (it enters the second product with 22 bits), all sums are fp32, the result is rounded
  * once.  K, N, rank and the row strides are multiples of 8 with
- * ldx >= K, ld_base >= N, ld_out >= N; rank <= 256; adapters * rank * K and adapters * rank * N below 2^40, M below 2^24,
+ * ldx >= K, ld_base >= N, ld_out >= N; rank <= 256; adapters * rank * K and adapters * rank * N below 2^40, M below 2^22,
  * M * N below 2^33 (else GPTQ_UNSUPPORTED_SHAPE).
  */
 GPTQ_API int gptq_w4a16_lora_add(const void *x, const void *a, const void *b, const void *scaling, const void *adapter,

@@ -18,14 +18,15 @@ int check_route(int M, int experts, int top_k)
     return GPTQ_OK;
 }
 
-// Sizes of a layer of experts.  A column tile of the output has an arrival counter: 65536 of 32 columns at least.
+// Sizes of a layer of experts.  (A column tile of the output has one of 65536 arrival counters; a launch stays under 2^32
+// threads.)
 int check_layer(int M, int hidden, int inter, int experts, int top_k, int group_size)
 {
     if (M <= 0 || hidden <= 0 || inter <= 0 || experts <= 0 || top_k <= 0 || group_size <= 0)
         return GPTQ_INVALID_ARG;
     if (experts > moe::kMaxExperts || top_k > moe::kMaxTopK || (long long)M * top_k > moe::kMaxPairs)
         return GPTQ_UNSUPPORTED_SHAPE;
-    if (group_size % 32 || hidden % group_size || inter % group_size || hidden > (1 << 20) || inter > (1 << 20))
+    if (group_size % 32 || hidden % group_size || inter % group_size || hidden > (1 << 18) || inter > (1 << 18))
         return GPTQ_UNSUPPORTED_SHAPE;
     // (32-bit byte offsets into the tokens and into the pairs' activations)
     if ((long long)M * hidden >= (1ll << 31) || (long long)M * top_k * inter >= (1ll << 31))
@@ -89,7 +90,7 @@ int check_lora(const void *x, const void *a, const void *b, const void *scaling,
         return GPTQ_INVALID_ARG;
     if (K % 8 || N % 8 || rank % 8 || ldx % 8 || ld_base % 8 || ld_out % 8 || rank > lora::kMaxRank || K >= (1 << 23) ||
         N >= (1 << 24) || (long long)adapters * rank * K >= (1ll << 40) || (long long)adapters * rank * N >= (1ll << 40) ||
-        M >= (1 << 24) || (long long)M * N >= (1ll << 33))  // (workgroups of a launch)
+        M >= (1 << 22) || (long long)M * N >= (1ll << 33))  // (threads of a launch)
         return GPTQ_UNSUPPORTED_SHAPE;
     if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(scaling) || !aligned16(adapter) || !aligned16(base) ||
         !aligned16(out))

@@ -167,6 +167,8 @@ def _rows(t, name):
     ld = t.stride(0) if rows > 1 else cols
     if ld < cols:
         raise ValueError(f"the rows of {name} overlap")
+    if ld > 2 ** 31 - 1:
+        raise ValueError(f"the rows of {name} stand too far apart")
     return t.data_ptr(), ld
 
 

@@ -372,3 +372,110 @@ def test_calls_through_the_extension_module_and_without_it_agree(S, monkeypatch)
     assert e.value.code == -2
     with pytest.raises(ValueError, match="out must be"):
         S.gptq_w4a16_moe(x, logits, gate_up, down, out[:, :64], top_k, group)
+
+
+# ---- scratch ----
+
+def test_scratch_of_the_caller(S):
+    """With a workspace of exactly the size asked for the calls run and give the same bits; with less they are refused, and
+    nothing is enqueued."""
+    from paper_2511_19438_amd import binding
+
+    rng = np.random.default_rng(21)
+    M, hidden, inter, E, top_k, group, rank = 20, 256, 128, 100, 3, 64, 16  # (grouped by a launch of its own)
+    gate_up, down = (tuple(map(cuda, t)) for t in layer(rng, hidden, inter, E, group))
+    x, logits = cuda(rng.standard_normal((M, hidden)).astype(np.float16)), cuda(rng.standard_normal((M, E)).astype(np.float32))
+    packed = tuple(map(cuda, random_packed(rng, hidden, inter, group)))
+    a, b, scaling = map(cuda, adapters(rng, 3, rank, hidden, inter))
+    adapter = cuda(rng.integers(-1, 3, M).astype(np.int32))
+
+    def moe(out):
+        return S.gptq_w4a16_moe(x, logits, gate_up, down, out, top_k, group)
+
+    def product(out):
+        return S.gptq_w4a16_gemm_lora(x, *packed, a, b, scaling, adapter, out, group)
+
+    base = torch.randn(M, inter, device="cuda").half()
+
+    def add(out):
+        return S.gptq_w4a16_lora_add(x, a, b, scaling, adapter, base, out)
+
+    for call, cols, need in [(moe, hidden, S.gptq_w4a16_moe_workspace_bytes(M, hidden, inter, E, top_k, group)),
+                             (product, inter, S.gptq_w4a16_lora_workspace_bytes(M, hidden, inter, rank, group)),
+                             (add, inter, S.gptq_w4a16_lora_workspace_bytes(M, hidden, inter, rank))]:
+        want = call(torch.empty(M, cols, dtype=torch.float16, device="cuda")).clone()
+        buf = torch.empty(need, dtype=torch.uint8, device="cuda")
+        try:
+            binding.gptq_w4a16_set_workspace(buf)
+            for _ in range(3):
+                got = call(torch.full((M, cols), float("nan"), dtype=torch.float16, device="cuda"))
+                assert torch.equal(got, want)
+            if call is not product:  # (a product may do with less)
+                binding.gptq_w4a16_set_workspace(buf[:need - 256])
+                out = torch.full((M, cols), 7.0, dtype=torch.float16, device="cuda")
+                with pytest.raises(binding.GptqError) as e:
+                    call(out)
+                assert e.value.code == -5
+                assert bool((out == 7).all())
+        finally:
+            binding.gptq_w4a16_set_workspace(None)
+
+
+def test_scratch_does_not_grow_under_capture(S):
+    from paper_2511_19438_amd import binding
+
+    rng = np.random.default_rng(22)
+    M, hidden, inter, E, top_k, group = 64, 128, 64, 4, 4, 32
+    gate_up, down = (tuple(map(cuda, t)) for t in layer(rng, hidden, inter, E, group))
+    x, logits = cuda(rng.standard_normal((M, hidden)).astype(np.float16)), cuda(rng.standard_normal((M, E)).astype(np.float32))
+    out = torch.full((M, hidden), 7.0, dtype=torch.float16, device="cuda")
+    binding.gptq_w4a16_set_workspace(None)  # no scratch at all
+    codes = []
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out.add_(1)
+        try:
+            S.gptq_w4a16_moe(x, logits, gate_up, down, out, top_k, group)
+        except binding.GptqError as e:
+            codes.append(e.code)
+    assert codes == [-5]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert bool((out == 8).all())
+
+
+def test_the_example_s_step(S):
+    """Projections with adapters and a layer of experts together, eagerly and in a graph, and the same step from its parts in
+    64 bits."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_layer.py")
+    spec = importlib.util.spec_from_file_location("decode_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    for batch in (1, 5, 40):
+        eager, out, _ = example.run(batch, 256, 384, 6, 2, 3, 8, steps=3)
+        assert torch.equal(eager, out) and bool(torch.isfinite(out).all())
+    step = example.Layer(4, 256, 384, 6, 2, 3, 8, seed=5)
+    x = torch.randn(4, 256, device="cuda").half()
+    adapter = torch.tensor([0, -1, 2, 2], dtype=torch.int32, device="cuda")
+    got = step.step(x, adapter).cpu().numpy().astype(np.float64)
+    to = lambda ts: [t.cpu().numpy() for t in ts]  # noqa: E731
+    from tests.serving_reference import dequant64
+
+    def rounded_norm(v):
+        return (v / np.sqrt(np.mean(v ** 2, 1, keepdims=True) + 1e-5)).astype(np.float16).astype(np.float64)
+
+    def projection(v, packed, parts):
+        w = v @ dequant64(*to(packed))
+        return lora64(v, *to(parts), adapter.cpu().numpy(), w)[0]
+
+    v = x.cpu().numpy().astype(np.float64)
+    qkv = projection(rounded_norm(v), step.qkv, step.qkv_adapters)
+    v = v + projection(qkv[:, 512:], step.o, step.o_adapters)
+    h = rounded_norm(v)
+    ids, weights = route64(h @ step.router.cpu().numpy().astype(np.float64), 2, True)
+    want = v + experts64(h, ids, weights, to(step.gate_up), to(step.down))[0]
+    # a dozen roundings to fp16 on the way, 2^-11 each; the routing weights move with the logits
+    assert np.linalg.norm(got - want) <= 12 * U16 * np.linalg.norm(want)
