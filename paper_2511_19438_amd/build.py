@@ -31,6 +31,7 @@ COMMON = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc"
 
 DECODE_BATCHES = (1, 2, 4, 8, 16)
 PREFILL_TILES = (1, 3, 5, 8, 9, 10, 11, 12, 13, 14)
+ADAPTER_TILES = PREFILL_TILES[1:]  # that can add low-rank adapters to their sums
 RING_GROUPS = (1, 2, 4)
 EXPERTS_SCALINGS = (0, 1, 2)
 
@@ -59,6 +60,8 @@ def units():
                         [f"-DGPTQ_EXPERTS_SCALING={s}", f"-DGPTQ_EXPERTS_DOWN={d}"]))
     for t in PREFILL_TILES:
         out.append(("prefill_tile.hip", f"prefill_tile{t}.o", [f"-DGPTQ_PREFILL_TILE={t}"]))
+    for t in ADAPTER_TILES:
+        out.append(("prefill_tile.hip", f"prefill_tile{t}_adapters.o", [f"-DGPTQ_PREFILL_TILE={t}", "-DGPTQ_PREFILL_ADAPTERS"]))
     return out
 
 

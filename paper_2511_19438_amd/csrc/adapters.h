@@ -21,6 +21,8 @@ struct Call {
 
 // Bytes of scratch of a call: x A^T of every row, in K slices.
 size_t scratch_bytes(int M, int K, int rank);
+// The first product alone, x A^T, for a product that adds the second to its own sums: `beside` says where it is.
+hipError_t launch_first(const Call &c, void *scratch, Beside &beside, hipStream_t stream);
 hipError_t launch_lora(const Call &c, void *scratch, hipStream_t stream);
 
 }  // namespace lora

@@ -406,7 +406,7 @@ int k_slices(int M, int K)
 }
 
 template <int TILES, int WAVES>
-void launch_shrink(const Args &a, hipStream_t stream)
+void launch_shrink_tiles(const Args &a, hipStream_t stream)
 {
     const int chunks = (a.rank + 16 * TILES - 1) / (16 * TILES);
     shrink_kernel<TILES, WAVES><<<dim3(a.row_tiles, a.slices, a.slots * chunks), 64 * WAVES, 0, stream>>>(a);
@@ -440,14 +440,15 @@ void launch_expand(const Args &a, hipStream_t stream)
         expand_kernel<8><<<grid, kThreads, 0, stream>>>(a);
 }
 
-}  // namespace
-
-size_t scratch_bytes(int M, int K, int rank)
+void launch_shrink(const Args &a, hipStream_t stream)
 {
-    return (size_t)k_slices(M, K) * M * rank * sizeof(float);
+    if (a.M <= 64 || a.rank <= 16)
+        launch_shrink_tiles<1, 4>(a, stream);
+    else
+        launch_shrink_tiles<2, 4>(a, stream);
 }
 
-hipError_t launch_lora(const Call &c, void *scratch, hipStream_t stream)
+Args args_of(const Call &c, void *scratch)
 {
     Args a = {};
     a.x = c.x;
@@ -471,10 +472,28 @@ hipError_t launch_lora(const Call &c, void *scratch, hipStream_t stream)
     const int steps = (c.K + 31) / 32;
     a.slices = k_slices(c.M, c.K);
     a.slice_steps = (steps + a.slices - 1) / a.slices;
-    if (c.M <= 64 || c.rank <= 16)
-        launch_shrink<1, 4>(a, stream);
-    else
-        launch_shrink<2, 4>(a, stream);
+    return a;
+}
+
+}  // namespace
+
+size_t scratch_bytes(int M, int K, int rank)
+{
+    return (size_t)k_slices(M, K) * M * rank * sizeof(float);
+}
+
+hipError_t launch_first(const Call &c, void *scratch, Beside &beside, hipStream_t stream)
+{
+    const Args a = args_of(c, scratch);
+    launch_shrink(a, stream);
+    beside = {a.t, a.b, a.scaling, a.adapter, a.rank, a.adapters, a.slices};
+    return hipGetLastError();
+}
+
+hipError_t launch_lora(const Call &c, void *scratch, hipStream_t stream)
+{
+    Args a = args_of(c, scratch);
+    launch_shrink(a, stream);
     if (row_by_row(c.M, c.N, c.rank)) {
         launch_expand_rows<1>(a, stream);
     } else {

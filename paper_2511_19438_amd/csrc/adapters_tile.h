@@ -1,0 +1,171 @@
+// The second product of low-rank adapters, s t B^T, added to the sums of an output tile while they are in registers
+// (gptq_w4a16_gemm_lora on the big-tile kernel).
+//
+// The output is then written once and rounded once, where a kernel after the product reads it, adds and rounds again (512 rows
+// of 12288 columns, 8 adapters of rank 32: that kernel takes 12 us; the tiles take 58.4 us without adapters and 65.6 with them).
+// t, in fp32 from the first product, comes to LDS 32 ranks at a time as the sum of two fp16 numbers, after a power of two
+// has brought the largest of a row's 32 to [1, 2): what is lost is 2^-22 of that largest.  B goes from memory to the operand
+// registers, that of the next adapter while one is multiplied.  A wavefront goes through the adapters that its rows have,
+// and multiplies the 16-row blocks that have rows of it; a row takes its values by selection, so that nothing of another
+// row's or adapter's reaches it.
+#pragma once
+
+#include "kernels.h"
+
+namespace gptq {
+namespace lora {
+
+constexpr int kTileRanks = 32;
+
+template <int BM>
+struct TileOperand {
+    half_t hi[BM][kTileRanks + 8], lo[BM][kTileRanks + 8];
+    float factor[BM];  // scaling and the power of two
+    int owner[BM];     // the row's adapter, -1 for none
+};
+
+// t of ranks r0 .. r0 + 31 of the tile's rows, by all threads of the workgroup: eight to a row, four ranks each.
+template <int BM, int THREADS>
+__device__ __forceinline__ void bring_t(const Beside &s, TileOperand<BM> &o, int r0, int m0, int M)
+{
+    static_assert(BM * 8 % 64 == 0, "whole wavefronts have rows");
+    const int part = threadIdx.x & 7, r = r0 + 4 * part;
+    const size_t step = (size_t)M * s.rank;
+    for (int row = threadIdx.x >> 3; row < BM; row += THREADS / 8) {
+        int l = m0 + row < M ? s.adapter[m0 + row] : -1;
+        l = l >= 0 && l < s.adapters ? l : -1;
+        float4_t t = {0.f, 0.f, 0.f, 0.f};
+        if (l >= 0 && r < s.rank) {
+            const float *src = s.t + (size_t)(m0 + row) * s.rank + r;
+            for (int i0 = 0; i0 < s.slices; i0 += 4) {  // (the sums of the slices, in their order)
+                float4_t v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[i] = *reinterpret_cast<const float4_t *>(src + min(i0 + i, s.slices - 1) * step);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i0 + i < s.slices)
+                        t += v[i];
+            }
+        }
+        uint32_t largest = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t bits = __builtin_bit_cast(uint32_t, t[j]) & 0x7fffffffu;
+            largest = bits > largest ? bits : largest;
+        }
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) {
+            const uint32_t other = __shfl_xor(largest, d);
+            largest = other > largest ? other : largest;
+        }
+        const int exponent = (int)(largest >> 23);  // (infinities and NaN go through as they are)
+        const int shift = exponent == 255 || largest == 0 ? 0 : exponent - 127;
+        half4_t hi, lo;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float v = ldexpf(t[j], -shift);
+            hi[j] = (half_t)v;
+            lo[j] = exponent == 255 ? (half_t)0.f : (half_t)(v - (float)hi[j]);
+        }
+        *reinterpret_cast<half4_t *>(&o.hi[row][4 * part]) = hi;
+        *reinterpret_cast<half4_t *>(&o.lo[row][4 * part]) = lo;
+        if (part == 0) {
+            o.factor[row] = l >= 0 ? ldexpf(s.scaling[l], shift) : 0.f;
+            o.owner[row] = l;
+        }
+    }
+}
+
+// All threads of the workgroup come here; those of `member` wavefronts hold sums: register r of block i, n-block t is row
+// row0 + 16 i + 4 (lane / 16) + r of the tile and column col + t of the output, as lane % 16 has it.  `smem`: LDS that is free.
+template <int BM, int THREADS, int TM, int TN>
+__device__ __forceinline__ void add_adapters(float4_t (&acc)[TM][TN], const Beside &s, unsigned char *smem, int m0, int row0,
+                                             int col, int M, int N, int lane, bool member)
+{
+    constexpr int WORDS = (16 * TM + 63) / 64;  // of 64 rows
+    TileOperand<BM> &o = *reinterpret_cast<TileOperand<BM> *>(smem);
+    const int lj = lane & 15, kg = lane >> 4;
+    const half_t *const column = s.b + (size_t)min(col, N - TN) * s.rank;  // (columns past the last are not stored)
+    for (int r0 = 0; r0 < s.rank; r0 += kTileRanks) {
+        __syncthreads();
+        bring_t<BM, THREADS>(s, o, r0, m0, M);
+        __syncthreads();
+        if (!member)
+            continue;
+        int mine[WORDS];
+        unsigned long long left[WORDS];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            mine[w] = 64 * w + lane < 16 * TM ? o.owner[row0 + 64 * w + lane] : -1;
+            left[w] = __ballot(mine[w] >= 0);
+        }
+        auto next = [&](unsigned long long (&rows)[WORDS]) {  // the first adapter that is left; all of its rows leave
+            int l = -1;
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w)
+                if (l < 0 && left[w] != 0)
+                    l = __builtin_amdgcn_readlane(mine[w], __builtin_ctzll(left[w]));
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) {
+                rows[w] = l < 0 ? 0 : __ballot(mine[w] == l);
+                left[w] &= ~rows[w];
+            }
+            return l;
+        };
+        const int r = r0 + 8 * kg;
+        auto load = [&](int l, half8_t (&bv)[TN]) {
+            const half_t *src = column + (size_t)l * N * s.rank + min(r, s.rank - 8);
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+                bv[t] = *reinterpret_cast<const half8_t *>(src + t * s.rank);
+        };
+        unsigned long long rows[WORDS];
+        half8_t bv[TN];
+        int l = next(rows);
+        if (l >= 0)
+            load(l, bv);
+        while (l >= 0) {
+            unsigned long long rows_after[WORDS];
+            half8_t after[TN] = {};
+            const int l_after = next(rows_after);
+            if (l_after >= 0)
+                load(l_after, after);
+#pragma unroll
+            for (int t = 0; t < TN; ++t)  // (ranks past the last: zeros)
+                bv[t] = r < s.rank ? bv[t] : half8_t{};
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                if (((rows[i / 4] >> (16 * (i % 4))) & 0xffff) == 0)
+                    continue;
+                const int row = row0 + 16 * i;
+                const half8_t hi = *reinterpret_cast<const half8_t *>(&o.hi[row + lj][8 * kg]);
+                const half8_t lo = *reinterpret_cast<const half8_t *>(&o.lo[row + lj][8 * kg]);
+                const float4_t factor = *reinterpret_cast<const float4_t *>(&o.factor[row + 4 * kg]);
+                bool chosen[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    chosen[q] = o.owner[row + 4 * kg + q] == l;
+#pragma unroll
+                for (int t = 0; t < TN; ++t) {
+                    float4_t d = {0.f, 0.f, 0.f, 0.f};
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, bv[t], d, 0, 0, 0);
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, bv[t], d, 0, 0, 0);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        acc[i][t][q] = chosen[q] ? __builtin_fmaf(factor[q], d[q], acc[i][t][q]) : acc[i][t][q];
+                }
+            }
+            l = l_after;
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+                bv[t] = after[t];
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w)
+                rows[w] = rows_after[w];
+        }
+    }
+}
+
+}  // namespace lora
+}  // namespace gptq

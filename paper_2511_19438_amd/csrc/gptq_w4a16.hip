@@ -549,12 +549,24 @@ int gptq::check_gemm(const void *x, const void *qweight, const void *qzeros, con
     return make_problem(x, qweight, qzeros, scales, nullptr, out, M, K, N, group_size, nullptr, p);
 }
 
-int gptq::run_gemm_with_tail(const Problem &p, size_t tail_bytes, hipStream_t stream, void **tail)
+bool gptq::gemm_takes_adapters(const Problem &p)
+{
+    const Resolved r = resolve(p, nullptr);
+    return !r.act && (r.kernel == 2 || r.big) && prefill_takes_adapters(p, r.prefill);
+}
+
+int gptq::run_gemm_between(const Problem &p, size_t tail_bytes, hipStream_t stream, int (*before)(void *, void *),
+                           int (*after)(void *, void *), void *context)
 {
     Resolved r = resolve(p, nullptr);
     Scratch scratch;
-    const int rc = acquire_with_tail(p, r, tail_bytes, stream, &scratch, tail);
-    return rc == GPTQ_OK ? launch_resolved(p, r, scratch, stream) : rc;
+    void *tail = nullptr;
+    int rc = acquire_with_tail(p, r, tail_bytes, stream, &scratch, &tail);
+    if (rc == GPTQ_OK)
+        rc = before(context, tail);
+    if (rc == GPTQ_OK)
+        rc = launch_resolved(p, r, scratch, stream);
+    return rc == GPTQ_OK ? after(context, tail) : rc;
 }
 
 extern "C" {

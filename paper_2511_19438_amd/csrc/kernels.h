@@ -14,6 +14,19 @@ typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
+namespace lora {
+
+// The adapters that a product adds to its sums, after x A^T of every row has been made.
+struct Beside {
+    const float *t;          // [slices, M, rank]: x A^T in parts, of the rows that have an adapter
+    const half_t *b;         // [adapters, N, rank]
+    const float *scaling;    // [adapters]
+    const int32_t *adapter;  // [M]
+    int rank, adapters, slices;
+};
+
+}  // namespace lora
+
 struct Problem {
     const half_t *x;          // [M, K]
     const uint32_t *qweight;  // [K/8, N]
@@ -23,6 +36,7 @@ struct Problem {
     const int32_t *x_perm = nullptr;  // [K]: gather x through it while staging (vector kernel, M = 1 only)
     half_t *out;              // [M, N]
     int M, K, N, group_size;
+    const lora::Beside *beside = nullptr;  // (big-tile pipelined kernel only)
 };
 
 // Whether the HBM-bound kernels - the vector kernel at one row, the small-batch kernel up to 16 - read a call's packed
@@ -142,6 +156,8 @@ struct PrefillPlan {
 bool prefill_supported(const Problem &p);
 // Whether the pipelined kernel (tiles, K slices) takes the problem; else the general path does.
 bool prefill_pipelined(const Problem &p);
+// Whether the plan's kernel can add adapters to its sums.
+bool prefill_takes_adapters(const Problem &p, const PrefillPlan &plan);
 bool prefill_tile_exists(int tile);  // the tile ids a plan may name
 void prefill_make_plan(const Problem &p, PrefillPlan &plan);
 // Estimated duration (microseconds) of a plan of the pipelined kernel.

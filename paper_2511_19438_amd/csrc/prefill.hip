@@ -298,6 +298,11 @@ void prefill_make_plan(const Problem &p, PrefillPlan &plan)
     plan.split_k = best_split;
 }
 
+bool prefill_takes_adapters(const Problem &p, const PrefillPlan &plan)
+{
+    return prefill_pipelined(p) && !plan.serial && plan.tile != 1;  // (256x256: the sums leave too few registers)
+}
+
 double prefill_estimate_us(const Problem &p, const PrefillPlan &plan)
 {
     return estimate_us(plan.tile, pace_of(plan.tile, plan.rows), grid_of(p, plan.tile, plan.rows), slices_of(p, plan.split_k),
@@ -329,6 +334,7 @@ hipError_t launch_prefill(const Problem &p, const PrefillPlan &plan, void *works
     a.stages_per_slice = 0;
     a.serial_slices = 0;
     a.serial_kw = 1;
+    a.beside = p.beside ? *p.beside : lora::Beside{};
     a.counters = reinterpret_cast<unsigned *>(workspace);
     a.partial = workspace ? reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + kCounterBytes) : nullptr;
     if (a.split_k > 1 && (size_t)ceil_div_i(p.M, plan.rows) *

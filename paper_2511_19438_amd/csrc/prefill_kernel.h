@@ -49,6 +49,7 @@
 
 #include <type_traits>
 
+#include "adapters_tile.h"
 #include "exchange.h"
 #include "kernels.h"
 #include "lds_dma.h"
@@ -82,6 +83,7 @@ struct Args {
     unsigned *counters;     // [tiles], zero between launches
     // SERIAL only: the slices that a workgroup walks (split_k is 1), and the wavefront groups that would have shared each
     int serial_slices, serial_kw;
+    lora::Beside beside;  // ADAPTERS only
 };
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -231,8 +233,8 @@ __device__ __forceinline__ void store_blocks(const float4_t (&acc)[TM][TN], half
 // Returns false in the workgroups that are not the last of their tile.  Partial layout:
 // [split_k][tiles][ACC / 2 pairs][256 threads] x 8 bytes.
 // `member`: whether this thread holds values (a workgroup of two K halves: only the first half's threads do; the
-// others only pass the barriers).
-template <int ACC>
+// others only pass the barriers, and unless `ALL` are told false).
+template <int ACC, bool ALL = false>
 __device__ __forceinline__ bool combine_slices(float (&v)[ACC], const Args &a, int slice, int tile_id, int tid,
                                                bool member)
 {
@@ -259,8 +261,10 @@ __device__ __forceinline__ bool combine_slices(float (&v)[ACC], const Args &a, i
     if (threadIdx.x == 0)
         s_last = (slice_arrive(a.counters + tile_id) == (unsigned)(a.split_k - 1));
     __syncthreads();
-    if (!s_last || !member)
+    if (!s_last || (!ALL && !member))
         return false;
+    if (ALL && !member)
+        return true;
     slice_acquire();
 #pragma unroll
     for (int e = 0; e < ACC; ++e)
@@ -356,7 +360,10 @@ constexpr int kWavesPerSimd = (BM * BN <= 128 * 256) ? 2 : 1;
 // slice that two wavefront groups would have shared, too - and adds their sums in the order of the sliced launch, so the
 // bits are those of that launch whatever its tile was.  For the 64x128 tile only, whose accumulators leave room for
 // the sums.  Slower than slices in parallel, and never chosen where scratch can be had.
-template <int BM, int BN, int WM, int WN, int BK, int NBUF, bool HALF = false, int KW = 1, bool SERIAL = false>
+//
+// ADAPTERS: the low-rank adapters of the rows are added to the sums before they are stored (adapters_tile.h).
+template <int BM, int BN, int WM, int WN, int BK, int NBUF, bool HALF = false, int KW = 1, bool SERIAL = false,
+          bool ADAPTERS = false>
 __global__ __launch_bounds__(kThreads * KW, (kWavesPerSimd<BM, BN>)) void prefill_pipelined_kernel(const Args a)
 {
     static_assert(KW == 1 || (KW == 2 && BM * BN <= 128 * 256), "two wavefronts per SIMD have 256 registers each");
@@ -884,7 +891,7 @@ __global__ __launch_bounds__(kThreads * KW, (kWavesPerSimd<BM, BN>)) void prefil
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     flat[(i * TN + t) * 4 + r] = acc[i][t][r];
-        if (!combine_slices<ACC>(flat, a, slice, tile_id, tid, kgroup == 0))
+        if (!combine_slices<ACC, ADAPTERS>(flat, a, slice, tile_id, tid, kgroup == 0))
             return;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -893,6 +900,10 @@ __global__ __launch_bounds__(kThreads * KW, (kWavesPerSimd<BM, BN>)) void prefil
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     acc[i][t][r] = flat[(i * TN + t) * 4 + r];
+    }
+    if constexpr (ADAPTERS) {
+        static_assert(sizeof(lora::TileOperand<BM>) <= KW * NBUF * L::BYTES, "t fits the rings");
+        lora::add_adapters<BM, KW * kThreads>(acc, a.beside, smem_all, m0, wm * WAVE_M, col_raw, M, N, lane, kgroup == 0);
     }
     if (kgroup == 0)
         store_blocks<TM, TN>(acc, a.out, m0 + wm * WAVE_M, col_raw, col_ok, kg, M, N);

@@ -1,5 +1,6 @@
 // Instantiates the MFMA kernels for ONE tile configuration (GPTQ_PREFILL_TILE, set on the compiler
-// command line) so that the configurations compile in parallel.
+// command line) so that the configurations compile in parallel; with GPTQ_PREFILL_ADAPTERS the instances that add the
+// rows' low-rank adapters.
 #include "prefill_kernel.h"
 
 #ifndef GPTQ_PREFILL_TILE
@@ -11,6 +12,10 @@ namespace prefill {
 
 template <int TILE>
 hipError_t launch_tile(const Args &a, int mode, int kw, hipStream_t stream);
+template <int TILE>
+hipError_t launch_tile_adapters(const Args &a, int mode, int kw, hipStream_t stream);
+template <>
+hipError_t launch_tile_adapters<GPTQ_PREFILL_TILE>(const Args &a, int mode, int kw, hipStream_t stream);
 
 namespace {
 
@@ -69,9 +74,37 @@ hipError_t launch(Kernel kernel, Args a, size_t lds, bool may_split, hipStream_t
 
 }  // namespace
 
+#ifdef GPTQ_PREFILL_ADAPTERS
+
+template <>
+hipError_t launch_tile_adapters<GPTQ_PREFILL_TILE>(const Args &a, int mode, int kw, hipStream_t stream)
+{
+    if (kw == 2 && mode == kGroupPerStage)
+        return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF2, false, 2, false, true>, a,
+                      2 * (size_t)NBUF2 * StageLayout<BM, BN, BK, false>::BYTES, true, stream, 2);
+    if (kw == 2 && mode == kGroupPerHalf)
+        return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF2, true, 2, false, true>, a,
+                      2 * (size_t)NBUF2 * StageLayout<BM, BN, BK, true>::BYTES, true, stream, 2);
+    if (kw == 1 && mode == kGroupPerStage)
+        return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF, false, 1, false, true>, a,
+                      (size_t)NBUF * StageLayout<BM, BN, BK, false>::BYTES, true, stream);
+    if (kw == 1 && mode == kGroupPerHalf)
+        return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF, true, 1, false, true>, a,
+                      (size_t)NBUF * StageLayout<BM, BN, BK, true>::BYTES, true, stream);
+    return hipErrorInvalidValue;
+}
+
+#else
+
 template <>
 hipError_t launch_tile<GPTQ_PREFILL_TILE>(const Args &a, int mode, int kw, hipStream_t stream)
 {
+#if GPTQ_PREFILL_TILE != 1
+    if (a.beside.t && a.serial_slices <= 1)
+        return launch_tile_adapters<GPTQ_PREFILL_TILE>(a, mode, kw, stream);
+#endif
+    if (a.beside.t)
+        return hipErrorInvalidValue;
 #if GPTQ_PREFILL_TILE != 1
     if (kw == 2 && mode == kGroupPerStage)
         return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF2, false, 2>, a,
@@ -107,6 +140,8 @@ hipError_t launch_tile<GPTQ_PREFILL_TILE>(const Args &a, int mode, int kw, hipSt
 #endif
     return hipErrorInvalidValue;
 }
+
+#endif
 
 }  // namespace prefill
 }  // namespace gptq

@@ -103,6 +103,37 @@ int status(hipError_t err)
     return err == hipSuccess ? GPTQ_OK : GPTQ_HIP_ERROR;
 }
 
+// A projection with adapters: their first product before it and the second in its tiles, or both after it.
+struct Projection {
+    lora::Call adapters;
+    lora::Beside beside;
+    bool in_tiles;
+    hipStream_t stream;
+};
+
+int before_product(void *context, void *t)
+{
+    Projection &c = *static_cast<Projection *>(context);
+    return c.in_tiles ? status(lora::launch_first(c.adapters, t, c.beside, c.stream)) : GPTQ_OK;
+}
+
+int after_product(void *context, void *t)
+{
+    const Projection &c = *static_cast<Projection *>(context);
+    return c.in_tiles ? GPTQ_OK : status(lora::launch_lora(c.adapters, t, c.stream));
+}
+
+// Whether a big tile adds the adapters itself: one rounding and a pass over the output less, but a tile goes through all the
+// adapters of its rows, where the kernel after the product has the chip for those of 16 rows each.  Prompts, whose rows share
+// one in turn, always gain, rows that alternate lose from 16 adapters on, and where K slices end in few tiles all do.  us, after
+// the product and in its tiles: 512 rows of 4096x12288 at rank 32 in runs of 48 rows 66.1, 62.4 (8 adapters), 67.7, 65.3 (32);
+// row by row 81.7, 78.6 (8), 96.3, 95.5 (16), 110.7, 128.5 (64); 1100 of 4096x4096 at rank 64, runs 80.5, 76.2, row by row
+// 152.0, 129.7 (8); 96 of 11008x4096 at rank 16, runs 30.3, 31.4 (4), row by row 30.8, 33.2 (4), 37.8, 46.4 (16).
+bool adapters_in_tiles(int M, int adapters)
+{
+    return adapters <= (M >= 128 ? 16 : 4);
+}
+
 }  // namespace
 
 extern "C" {
@@ -213,15 +244,12 @@ int gptq_w4a16_gemm_lora(const void *x, const void *qweight, const void *qzeros,
     rc = check_lora(x, a, b, scaling, adapter, out, out, M, K, N, rank, adapters, K, N, N);
     if (rc != GPTQ_OK)
         return rc;
-    const hipStream_t st = static_cast<hipStream_t>(stream);
-    void *t = nullptr;
-    rc = run_gemm_with_tail(p, lora::scratch_bytes(M, K, rank), st, &t);
-    if (rc != GPTQ_OK)
-        return rc;
-    const lora::Call c = {p.x, static_cast<const half_t *>(a), static_cast<const half_t *>(b),
-                          static_cast<const float *>(scaling), static_cast<const int32_t *>(adapter), p.out, p.out, M, K, N,
-                          rank, adapters, K, N, N};
-    return status(lora::launch_lora(c, t, st));
+    Projection c = {{p.x, static_cast<const half_t *>(a), static_cast<const half_t *>(b), static_cast<const float *>(scaling),
+                     static_cast<const int32_t *>(adapter), p.out, p.out, M, K, N, rank, adapters, K, N, N},
+                    {}, adapters_in_tiles(M, adapters) && gemm_takes_adapters(p), static_cast<hipStream_t>(stream)};
+    if (c.in_tiles)
+        p.beside = &c.beside;
+    return run_gemm_between(p, lora::scratch_bytes(M, K, rank), c.stream, before_product, after_product, &c);
 }
 
 size_t gptq_w4a16_lora_workspace_bytes(int M, int K, int N, int rank, int group_size)

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.serving_reference import U16, experts64, lora64, random_packed, route64
+from tests.serving_reference import U16, U32, dequant64, experts64, lora64, random_packed, route64
 
 pytestmark = pytest.mark.gpu
 
@@ -306,8 +306,8 @@ def test_lora_infinite_adapters_stay_with_their_rows(S):
     inside(got, want, off, "large sums")
 
 
-@pytest.mark.parametrize("M,K,N,group,rank,count", [(1, 512, 264, 128, 16, 3), (5, 256, 136, 64, 8, 5), (32, 1024, 520, 128, 16, 32),
-                                                    (40, 384, 264, 32, 24, 4), (200, 512, 264, 128, 32, 4)])
+# (the kernels of few rows; a big tile's adapters are added before its one rounding)
+@pytest.mark.parametrize("M,K,N,group,rank,count", [(1, 512, 264, 128, 16, 3), (5, 256, 136, 64, 8, 5), (32, 1024, 520, 128, 16, 32)])
 def test_gemm_lora_is_the_product_with_the_adapters_on_top(S, M, K, N, group, rank, count):
     from paper_2511_19438_amd import binding
 
@@ -322,6 +322,72 @@ def test_gemm_lora_is_the_product_with_the_adapters_on_top(S, M, K, N, group, ra
     binding.gptq_w4a16_gemm(cuda(x), *packed, None, base, group)
     want, off = lora64(x, a, b, scaling, adapter, base.cpu().numpy())
     inside(out.cpu().numpy(), want, off, "gemm_lora")
+
+
+# one row, small batches, the mid-batch kernel without and with K slices, the big tile (adapters in its tiles, too many for that,
+# with K slices, a wide one, several chunks of rank), the general path
+@pytest.mark.parametrize("M,K,N,group,rank,count", [
+    (1, 512, 264, 128, 16, 3), (5, 256, 136, 64, 8, 5), (32, 1024, 520, 128, 16, 32), (40, 384, 264, 32, 24, 4),
+    (60, 4096, 2048, 128, 16, 3), (72, 8192, 512, 128, 16, 4), (90, 11008, 4096, 128, 8, 3), (130, 512, 288, 128, 32, 40),
+    (200, 512, 264, 128, 32, 4), (129, 1024, 288, 128, 40, 4), (256, 4096, 512, 128, 16, 4), (300, 480, 288, 32, 8, 16),
+    (300, 480, 264, 96, 8, 5), (70, 352, 104, 8, 16, 3), (333, 2048, 4096, 64, 72, 5), (512, 1024, 4096, 128, 24, 1),
+    (1100, 512, 4096, 128, 16, 6), (240, 4096, 1024, 32, 256, 2)])
+def test_gemm_lora(S, M, K, N, group, rank, count):
+    """Rows without an adapter get the product; the others are, by definition in 64 bits, off by fp32 sums, by weights that a
+    kernel may round to fp16, by the rounding of the output and by that of the product before the adapters are added."""
+    from paper_2511_19438_amd import binding
+
+    rng = np.random.default_rng([M, K, N])
+    host = random_packed(rng, K, N, group)
+    packed = tuple(map(cuda, host))
+    a, b, scaling = adapters(rng, count, rank, K, N)
+    x = rng.standard_normal((M, K)).astype(np.float16)
+    adapter = rng.integers(-1, count, size=M).astype(np.int32)
+    adapter[rng.integers(0, M)] = count + 5  # (none, as well)
+    out = torch.full((M, N), float("nan"), dtype=torch.float16, device="cuda")
+    S.gptq_w4a16_gemm_lora(cuda(x), *packed, cuda(a), cuda(b), cuda(scaling), cuda(adapter), out, group)
+    got = out.cpu().numpy()
+    base = torch.empty_like(out)
+    binding.gptq_w4a16_gemm(cuda(x), *packed, None, base, group)
+    bare = (adapter < 0) | (adapter >= count)
+    np.testing.assert_array_equal(got[bare], base.cpu().numpy()[bare])
+    w = dequant64(*host)
+    product, absolute = x.astype(np.float64) @ w, np.abs(x.astype(np.float64)) @ np.abs(w)
+    want, off = lora64(x, a, b, scaling, adapter, product)
+    off = off + ((K + 16) * U32 + U16) * absolute + U16 * np.abs(product) + U16 * np.abs(want)
+    inside(got, want, off, "gemm_lora")
+    assert np.linalg.norm(got - want) <= 1.5 * U16 * np.linalg.norm(want)
+
+
+def test_adapters_in_tiles_keep_rows_apart(S):
+    """Infinities and NaN in one row's x, one adapter's A and one's B reach the rows that have them and no other; 300 rows of two
+    adapters, in blocks and in turn; sums past fp16's range in x A^T are no infinities."""
+    rng = np.random.default_rng(7)
+    M, K, N, group, rank, count = 300, 512, 288, 128, 16, 4
+    host = random_packed(rng, K, N, group)
+    packed = tuple(map(cuda, host))
+    a, b, scaling = adapters(rng, count, rank, K, N)
+    x = rng.standard_normal((M, K)).astype(np.float16)
+    for adapter in (np.arange(M, dtype=np.int32) % count, np.arange(M, dtype=np.int32) * count // M):
+        adapter = adapter.astype(np.int32)
+
+        def call(x, a, b, scaling):
+            out = torch.full((M, N), float("nan"), dtype=torch.float16, device="cuda")
+            S.gptq_w4a16_gemm_lora(cuda(x), *packed, cuda(a), cuda(b), cuda(scaling), cuda(adapter), out, group)
+            return out.cpu().numpy()
+
+        clean = call(x, a, b, scaling)
+        a2, b2, x2 = a.copy(), b.copy(), x.copy()
+        a2[1] = np.inf
+        b2[2] = np.nan
+        x2[17] = np.inf
+        dirty = call(x2, a2, b2, scaling)
+        touched = (adapter == 1) | (adapter == 2)
+        touched[17] = True
+        np.testing.assert_array_equal(dirty[~touched], clean[~touched])
+        assert not np.isfinite(dirty[touched]).any()
+        loud = call(x, (a.astype(np.float64) * 2.0 ** 18).astype(np.float16), b, scaling * np.float32(2.0 ** -18))
+        np.testing.assert_array_equal(loud, clean)  # (powers of two)
 
 
 # ---- marshalling ----
@@ -462,8 +528,6 @@ def test_the_example_s_step(S):
     adapter = torch.tensor([0, -1, 2, 2], dtype=torch.int32, device="cuda")
     got = step.step(x, adapter).cpu().numpy().astype(np.float64)
     to = lambda ts: [t.cpu().numpy() for t in ts]  # noqa: E731
-    from tests.serving_reference import dequant64
-
     def rounded_norm(v):
         return (v / np.sqrt(np.mean(v ** 2, 1, keepdims=True) + 1e-5)).astype(np.float16).astype(np.float64)
 
