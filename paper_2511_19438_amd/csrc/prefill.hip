@@ -300,7 +300,7 @@ void prefill_make_plan(const Problem &p, PrefillPlan &plan)
 
 bool prefill_takes_adapters(const Problem &p, const PrefillPlan &plan)
 {
-    return prefill_pipelined(p) && !plan.serial && plan.tile != 1;  // (256x256: the sums leave too few registers)
+    return prefill_pipelined(p) && plan.tile != 1;  // (256x256: the sums leave too few registers)
 }
 
 double prefill_estimate_us(const Problem &p, const PrefillPlan &plan)

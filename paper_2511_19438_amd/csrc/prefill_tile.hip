@@ -85,6 +85,16 @@ hipError_t launch_tile_adapters<GPTQ_PREFILL_TILE>(const Args &a, int mode, int 
     if (kw == 2 && mode == kGroupPerHalf)
         return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF2, true, 2, false, true>, a,
                       2 * (size_t)NBUF2 * StageLayout<BM, BN, BK, true>::BYTES, true, stream, 2);
+#if GPTQ_PREFILL_TILE == 5
+    if (a.serial_slices > 1 && mode == kGroupPerStage)
+        return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF, false, 1, true, true>, a,
+                      (size_t)NBUF * StageLayout<BM, BN, BK, false>::BYTES, false, stream);
+    if (a.serial_slices > 1 && mode == kGroupPerHalf)
+        return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF, true, 1, true, true>, a,
+                      (size_t)NBUF * StageLayout<BM, BN, BK, true>::BYTES, false, stream);
+#endif
+    if (a.serial_slices > 1)
+        return hipErrorInvalidValue;
     if (kw == 1 && mode == kGroupPerStage)
         return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF, false, 1, false, true>, a,
                       (size_t)NBUF * StageLayout<BM, BN, BK, false>::BYTES, true, stream);
@@ -99,12 +109,12 @@ hipError_t launch_tile_adapters<GPTQ_PREFILL_TILE>(const Args &a, int mode, int 
 template <>
 hipError_t launch_tile<GPTQ_PREFILL_TILE>(const Args &a, int mode, int kw, hipStream_t stream)
 {
-#if GPTQ_PREFILL_TILE != 1
-    if (a.beside.t && a.serial_slices <= 1)
-        return launch_tile_adapters<GPTQ_PREFILL_TILE>(a, mode, kw, stream);
-#endif
     if (a.beside.t)
+#if GPTQ_PREFILL_TILE != 1
+        return launch_tile_adapters<GPTQ_PREFILL_TILE>(a, mode, kw, stream);
+#else
         return hipErrorInvalidValue;
+#endif
 #if GPTQ_PREFILL_TILE != 1
     if (kw == 2 && mode == kGroupPerStage)
         return launch(prefill_pipelined_kernel<BM, BN, WM, WN, BK, NBUF2, false, 2>, a,

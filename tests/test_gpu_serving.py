@@ -487,6 +487,35 @@ def test_scratch_of_the_caller(S):
             binding.gptq_w4a16_set_workspace(None)
 
 
+@pytest.mark.parametrize("M,K,N,group", [(256, 4096, 512, 128), (72, 8192, 512, 128), (130, 8192, 264, 32)])
+def test_gemm_lora_without_scratch_for_its_slices(S, M, K, N, group):
+    """A workspace that holds x A^T but not the K slices of the product, whose tiles add the adapters: the call runs, slices one
+    after the other, with the same bits."""
+    from paper_2511_19438_amd import binding
+
+    rng = np.random.default_rng([M, K])
+    rank, count = 16, 4
+    packed = tuple(map(cuda, random_packed(rng, K, N, group)))
+    a, b, scaling = map(cuda, adapters(rng, count, rank, K, N))
+    x, adapter = cuda(rng.standard_normal((M, K)).astype(np.float16)), cuda(rng.integers(-1, count, M).astype(np.int32))
+
+    def call():
+        out = torch.full((M, N), float("nan"), dtype=torch.float16, device="cuda")
+        return S.gptq_w4a16_gemm_lora(x, *packed, a, b, scaling, adapter, out, group)
+
+    assert binding.gptq_w4a16_plan_query(M, K, N, group).split_k > 1
+    want = call().clone()
+    least, most = (S.gptq_w4a16_lora_workspace_bytes(M, K, N, rank, g) for g in (0, group))
+    assert least < most
+    buf = torch.empty(least, dtype=torch.uint8, device="cuda")
+    try:
+        binding.gptq_w4a16_set_workspace(buf)
+        for _ in range(2):
+            assert torch.equal(call(), want)
+    finally:
+        binding.gptq_w4a16_set_workspace(None)
+
+
 def test_scratch_does_not_grow_under_capture(S):
     from paper_2511_19438_amd import binding
 

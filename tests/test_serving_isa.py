@@ -71,7 +71,7 @@ def test_tiles_with_adapters_leave_registers_of_pending_lds_reads_alone(tile_fil
             for t in lines:
                 in_asm = t.startswith(";;#ASMSTART") or (in_asm and not t.startswith(";;#ASMEND"))
                 assert in_asm or not re.search(r"\bm0\b", t), f"{name}: {t}"
-    assert seen == 4 * len(B.ADAPTER_TILES)
+    assert seen == 4 * len(B.ADAPTER_TILES) + 2  # (slices one after the other on 64x128)
 
 
 def test_tiles_with_adapters_spill_nothing(tile_files):
