@@ -516,6 +516,33 @@ def test_gemm_lora_without_scratch_for_its_slices(S, M, K, N, group):
         binding.gptq_w4a16_set_workspace(None)
 
 
+def test_gemm_lora_in_a_graph(S):
+    """Replays of tiles that add adapters, in K slices and without, follow the rows' adapters; eager calls between them."""
+    rng = np.random.default_rng(31)
+    rank, count, group = 16, 4, 128
+    for M, K, N in [(256, 4096, 512), (300, 512, 288)]:
+        packed = tuple(map(cuda, random_packed(rng, K, N, group)))
+        a, b, scaling = map(cuda, adapters(rng, count, rank, K, N))
+        x, adapter = cuda(rng.standard_normal((M, K)).astype(np.float16)), cuda(rng.integers(-1, count, M).astype(np.int32))
+        out, eager = (torch.empty(M, N, dtype=torch.float16, device="cuda") for _ in range(2))
+
+        def call(to):
+            return S.gptq_w4a16_gemm_lora(x, *packed, a, b, scaling, adapter, to, group)
+
+        call(eager)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(out)
+        for i in range(4):
+            adapter.copy_(cuda(rng.integers(-1, count, M).astype(np.int32)))
+            out.fill_(float("nan"))
+            graph.replay()
+            call(eager)
+            torch.cuda.synchronize()
+            assert torch.equal(out, eager), i
+
+
 def test_scratch_does_not_grow_under_capture(S):
     from paper_2511_19438_amd import binding
 
